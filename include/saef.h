@@ -77,6 +77,18 @@ extern "C" {
 #define SAEF_VARIANT_EF 0   /* local error feedback: gradient taken at x_t (EF branch) */
 #define SAEF_VARIANT_SAEF 1 /* step ahead: gradient taken at x_t - e^(k)_t (SAEF branch) */
 
+/* element types of gradients and features */
+#define SAEF_F32 0
+#define SAEF_BF16 1
+#define SAEF_F16 2
+
+#define SAEF_ACT_NONE 0 /* y = z */
+#define SAEF_ACT_RELU 1 /* y = max(z, 0) */
+#define SAEF_ACT_SILU 2 /* y = z / (1 + exp(-z)) */
+
+#define SAEF_NORM_2 0   /* sqrt(sum g^2) */
+#define SAEF_NORM_INF 1 /* max |g| */
+
 typedef struct saef_layout saef_layout;
 
 /* Layer-wise compression needs one scale per tensor (Experiments: all
@@ -202,6 +214,94 @@ int saef_materialize(const saef_layout* layout, int32_t K, int32_t mode, const f
                      const float* e_srv, const float* x, const uint64_t* signs,
                      const float* scales, const uint64_t* srv_signs, const float* srv_scales,
                      float* e_out, float* e_srv_out, float* x_out, hipStream_t stream);
+
+/* ---------------------------------------------------------------- group norm
+ * The normalisation of a network whose K workers are simulated on one GPU,
+ * each at its own evaluation point xh[k].  (Batch norm's running statistics
+ * are no parameters: they are in no vector of Algorithm 1, travel in no
+ * message and would differ at the K points.)  Features are channels last: worker
+ * k's N samples of P pixels by C channels, contiguous (K, N, P, C).  Per
+ * sample and group of C / G consecutive channels, over its P C / G values:
+ *   mean, rstd = 1 / sqrt(var + eps)      (var without Bessel's correction)
+ *   z = gamma (x - mean) rstd + beta,  y = act(z)
+ * gamma and beta of worker k start at gamma + k ld and beta + k ld: ld = d_pad
+ * for parameters in the rows of xh (C contiguous values, ld >= C).
+ * Statistics are formed in binary64, the rest in fp32; y is rounded once, to
+ * dtype.  mean, rstd: (K, N, G), for the backward pass.
+ * A group norm is planned for one shape; the plan owns 16 bytes of device
+ * scratch per channel, sample and pixel range (saef_group_norm_create chooses how many
+ * of those a sample is cut into).  Calls that use one plan must not run
+ * concurrently.  K <= 4096, C <= 65536, G divides C, eps > 0. */
+typedef struct saef_group_norm saef_group_norm;
+
+int saef_group_norm_create(int32_t K, int64_t N, int64_t P, int32_t C, int32_t G, int32_t dtype,
+                           int32_t act, float eps, saef_group_norm** out);
+int saef_group_norm_destroy(saef_group_norm* plan);
+
+/* y must not overlap an input. */
+int saef_group_norm_forward(const saef_group_norm* plan, const void* x, const float* gamma,
+                            const float* beta, int64_t ld, void* y, float* mean, float* rstd,
+                            hipStream_t stream);
+
+/* The gradient: dx (as x) from dy, and worker k's dgamma and dbeta (C each,
+ * at dgamma + k ldg and dbeta + k ldg, e.g. in its gradient row; overwritten),
+ * summed over its samples in a fixed order.  x, gamma, beta as in the forward
+ * call, mean and rstd as it left them.  relu: the derivative at z <= 0 is 0.
+ * The outputs must not overlap the inputs or one another; rows of dgamma and
+ * dbeta may interleave. */
+int saef_group_norm_backward(const saef_group_norm* plan, const void* dy, const void* x,
+                             const float* gamma, const float* beta, int64_t ld,
+                             const float* mean, const float* rstd, void* dx, float* dgamma,
+                             float* dbeta, int64_t ldg, hipStream_t stream);
+
+/* ---------------------------------------------------------------- clipping
+ * Before the second half each worker may clip its own gradient to a global
+ * norm over all of its tensors (the server sees messages only):
+ *   norm_k = sqrt(sum_i g_ki^2)  or  max_i |g_ki|
+ *   c_k    = min(1, fp32(max_norm / fp32(norm_k + 1e-6)))
+ *   g_ki  <- fp32(c_k g_ki), rounded again to a 16-bit output
+ * Squares are exact in binary64 and summed there, in a fixed order of the
+ * library's own: norms are the same from run to run, and agree with the
+ * exact ones to within an fp32 rounding and n 2^-53.  An infinite value makes
+ * norm_k infinite and c_k 0; one that is no number makes norm_k and c_k none,
+ * and the worker's whole gradient with it, which the compression reports as
+ * SAEF_ERANGE.
+ *
+ * A saef_grads says where the gradients of K workers lie: ptr[k L + l] (host
+ * array, copied) is the device address of the n[l] contiguous elements of tensor l
+ * of worker k, of type dtype, aligned to an element: a row of the layout at
+ * off[l], a tensor that automatic differentiation filled, or a piece of a
+ * bucket.  No two may overlap; the memory must stay while the handle is
+ * used.  The handle owns 8 bytes of device scratch per (tile, worker), and
+ * per (tensor, worker) 16.  Calls that use one saef_grads must not run
+ * concurrently.  Synchronous; the layout must outlive the handle. */
+typedef struct saef_grads saef_grads;
+
+int saef_grads_create(const saef_layout* layout, int32_t K, int32_t dtype, void* const* ptr,
+                      saef_grads** out);
+int saef_grads_destroy(saef_grads* grads);
+
+/* norms (K, device): each worker's norm over all of its tensors;
+ * tensor_norms (K, L), may be NULL: of each tensor.  norm_type SAEF_NORM_2 or
+ * SAEF_NORM_INF. */
+int saef_grad_norm(const saef_grads* grads, int32_t norm_type, float* norms, float* tensor_norms,
+                   hipStream_t stream);
+
+/* Clips every worker's gradient to max_norm (finite, at least 0), given norms
+ * (K).  out: (K, d_pad) fp32 rows of the layout that receive c_k g_k (padding
+ * is not written), the gradients themselves are left; out == NULL: in place,
+ * rounded to their own type (a worker with c_k = 1 is not touched). */
+int saef_clip(const saef_grads* grads, float max_norm, const float* norms, float* out,
+              hipStream_t stream);
+
+/* saef_round_end on clipped gradients: exactly saef_clip(max_norm, norms) of
+ * the rows g followed by saef_round_end, without a pass over g of its own; g is only
+ * read.  norms: (K), must not overlap what the call writes. */
+int saef_round_end_clipped(const saef_layout* layout, int64_t t, int64_t period, int32_t K,
+                           float lr, float mu, int32_t mode, float max_norm, const float* norms,
+                           const float* g, float* m, float* e, float* e_srv, float* x,
+                           uint64_t* signs, float* scales, uint64_t* srv_signs,
+                           float* srv_scales, hipStream_t stream);
 
 /* ---------------------------------------------------------------- Top-K
  * The paper's second compressor (Experiments: Top-K sparsification with the

@@ -12,6 +12,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = [os.path.join(HERE, "csrc", f) for f in ("saef_kernels.hip", "saef_topk.hip",
+                                                          "saef_clip.hip", "saef_group_norm.hip",
                                                           "saef_api.hip")]
 LIB = os.path.join(HERE, "libsaef.so")
 # the same library with larger work tiles: the tile-size determinism tests run

@@ -7,9 +7,12 @@
 #include <initializer_list>
 #include <mutex>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "saef.h"
+#include "saef_clip.h"
+#include "saef_group_norm.h"
 #include "saef_internal.h"
 #include "saef_topk.h"
 
@@ -71,6 +74,28 @@ struct saef_topk {
   saef::TkStreams side{};
   saef::TkPart all{};               // every tensor
   std::vector<saef::TkPart> pipe;   // the iteration end's parts (empty: not pipelined)
+};
+
+// Where K workers' gradients lie, and the scratch of their norms.
+struct saef_grads {
+  const saef_layout* layout = nullptr;
+  int32_t K = 0;
+  int32_t dtype = 0;
+  // the tensors' memory, in order of address (none overlap)
+  std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+  saef::GradsDev dev{};
+  void* mem_ptr = nullptr;
+  void* mem_part = nullptr;
+  void* mem_tpart = nullptr;
+};
+
+// The shape of a group norm and the scratch of its sums.
+struct saef_group_norm {
+  int device = 0;
+  int32_t dtype = 0;
+  int32_t act = 0;
+  saef::GroupNormDev dev{};
+  void* mem_part = nullptr;
 };
 
 namespace {
@@ -199,6 +224,9 @@ int check_common(const saef_layout* lay, int32_t K) {
   if (dev != lay->device) return SAEF_EINVAL;
   return SAEF_OK;
 }
+
+// What gradients may be clipped to.
+bool clip_bound_ok(float max_norm) { return std::isfinite(max_norm) && max_norm >= 0.0f; }
 
 bool f32_ok(const float* p) { return p != nullptr && aligned(p, 4); }
 bool u64_ok(const uint64_t* p) { return p != nullptr && aligned(p, 8); }
@@ -394,6 +422,16 @@ int compress_impl(const saef_layout* layout, int32_t K, float lr, float mu, cons
                                          fold, stream));
 }
 
+// [p, p + bytes) shares memory with one of the gradients?
+bool meets_grads(const saef_grads* g, const void* p, size_t bytes) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+  // the first gradient that ends after p
+  const auto it = std::upper_bound(
+      g->spans.begin(), g->spans.end(), a,
+      [](uintptr_t v, const std::pair<uintptr_t, uintptr_t>& s) { return v < s.second; });
+  return it != g->spans.end() && it->first < a + bytes;
+}
+
 bool mu_ok(float mu) { return mu >= 0.0f && mu < 1.0f; }
 
 }  // namespace
@@ -535,7 +573,7 @@ int round_end_impl(const saef_layout* layout, int64_t t, int64_t period, int32_t
                    float mu, int32_t mode, const float* g, float* m, float* e, float* e_srv,
                    float* x, uint64_t* signs, float* scales, uint64_t* srv_signs,
                    float* srv_scales, hipStream_t stream, const DevLayout* dev = nullptr,
-                   float* xh = nullptr) {
+                   float* xh = nullptr, float max_norm = 0.0f, const float* norms = nullptr) {
   int rc = check_common(layout, K);
   if (rc != SAEF_OK) return rc;
   if (t < 0 || period < 0 || !std::isfinite(lr)) return SAEF_EINVAL;
@@ -550,6 +588,16 @@ int round_end_impl(const saef_layout* layout, int64_t t, int64_t period, int32_t
   if (m != nullptr && (!f32_ok(m) || overlap(m, vb, g, vb) || overlap(m, vb, e, vb) ||
                        overlap(m, vb, x, xb)))
     return SAEF_EINVAL;
+  if (norms != nullptr) {
+    // read while all of these are written
+    const size_t wb = (size_t)layout->d_pad / 64 * sizeof(uint64_t);
+    const size_t sb = (size_t)layout->L * sizeof(float);
+    if (!aligned(norms, 4) || !clip_bound_ok(max_norm) ||
+        overlap_any(norms, K * sizeof(float),
+                    {{e, vb}, {m, vb}, {x, xb}, {signs, K * wb}, {scales, K * sb}, {e_srv, xb},
+                     {srv_signs, wb}, {srv_scales, sb}}))
+      return SAEF_EINVAL;
+  }
 
   const bool pending = t > 0;
   const bool averaging = period > 0 && (t + 1) % period == 0;
@@ -561,7 +609,7 @@ int round_end_impl(const saef_layout* layout, int64_t t, int64_t period, int32_t
       return saef::launch_worker(d, K, lr, mu, g, m, e, signs, scales, pending, x, srv_signs,
                                  srv_scales, pending && dc, xh, stream, ev);
     return saef::launch_compress(d, K, lr, mu, g, m, e, signs, scales, pending && !averaging,
-                                 stream, ev);
+                                 stream, ev, max_norm, norms);
   }));
   if (rc != SAEF_OK) return rc;
   // Small layouts: the aggregation adds up the worker partials itself, one
@@ -684,6 +732,104 @@ int saef_round_end(const saef_layout* layout, int64_t t, int64_t period, int32_t
   if (m == nullptr ? mu != 0.0f : !mu_ok(mu)) return SAEF_EINVAL;
   return round_end_impl(layout, t, period, K, lr, mu, mode, g, m, e, e_srv, x, signs, scales,
                         srv_signs, srv_scales, stream);
+}
+
+int saef_round_end_clipped(const saef_layout* layout, int64_t t, int64_t period, int32_t K,
+                           float lr, float mu, int32_t mode, float max_norm, const float* norms,
+                           const float* g, float* m, float* e, float* e_srv, float* x,
+                           uint64_t* signs, float* scales, uint64_t* srv_signs,
+                           float* srv_scales, hipStream_t stream) {
+  if (m == nullptr ? mu != 0.0f : !mu_ok(mu)) return SAEF_EINVAL;
+  if (norms == nullptr) return SAEF_EINVAL;
+  return round_end_impl(layout, t, period, K, lr, mu, mode, g, m, e, e_srv, x, signs, scales,
+                        srv_signs, srv_scales, stream, nullptr, nullptr, max_norm, norms);
+}
+
+int saef_grads_create(const saef_layout* layout, int32_t K, int32_t dtype, void* const* ptr,
+                      saef_grads** out) {
+  if (out == nullptr) return SAEF_EINVAL;
+  *out = nullptr;
+  int rc = check_common(layout, K);
+  if (rc != SAEF_OK) return rc;
+  if (ptr == nullptr || dtype < SAEF_F32 || dtype > SAEF_F16) return SAEF_EINVAL;
+  const size_t es = (size_t)saef::dtype_bytes(dtype);
+  const size_t rows = (size_t)K * layout->L;
+  saef_grads* g = nullptr;
+  try {
+    g = new saef_grads();
+    for (size_t i = 0; i < rows; ++i) {
+      if (ptr[i] == nullptr || !aligned(ptr[i], es)) {
+        delete g;
+        return SAEF_EINVAL;
+      }
+      const uintptr_t a = reinterpret_cast<uintptr_t>(ptr[i]);
+      g->spans.emplace_back(a, a + es * (size_t)layout->n[i % layout->L]);
+    }
+    std::sort(g->spans.begin(), g->spans.end());
+  } catch (const std::bad_alloc&) {
+    delete g;
+    return SAEF_EHIP;
+  }
+  for (size_t i = 1; i < rows; ++i)
+    if (g->spans[i - 1].second > g->spans[i].first) {
+      delete g;
+      return SAEF_EINVAL;
+    }
+  g->layout = layout;
+  g->K = K;
+  g->dtype = dtype;
+  hipError_t err = hipMalloc(&g->mem_ptr, rows * sizeof(void*));
+  if (err == hipSuccess)
+    err = hipMalloc(&g->mem_part, (size_t)K * layout->dev.n_tiles * sizeof(double));
+  if (err == hipSuccess) err = hipMalloc(&g->mem_tpart, rows * sizeof(double));
+  if (err == hipSuccess)
+    err = hipMemcpy(g->mem_ptr, ptr, rows * sizeof(void*), hipMemcpyHostToDevice);
+  if (err != hipSuccess) {
+    (void)saef_grads_destroy(g);
+    return SAEF_EHIP;
+  }
+  g->dev = saef::GradsDev{static_cast<void* const*>(g->mem_ptr), static_cast<double*>(g->mem_part),
+                          static_cast<double*>(g->mem_tpart), K, dtype};
+  *out = g;
+  return SAEF_OK;
+}
+
+int saef_grads_destroy(saef_grads* grads) {
+  if (grads == nullptr) return SAEF_EINVAL;
+  for (void* q : {grads->mem_ptr, grads->mem_part, grads->mem_tpart}) (void)hipFree(q);
+  delete grads;
+  return SAEF_OK;
+}
+
+int saef_grad_norm(const saef_grads* grads, int32_t norm_type, float* norms, float* tensor_norms,
+                   hipStream_t stream) {
+  if (grads == nullptr) return SAEF_EINVAL;
+  int rc = check_common(grads->layout, grads->K);
+  if (rc != SAEF_OK) return rc;
+  if (norm_type != SAEF_NORM_2 && norm_type != SAEF_NORM_INF) return SAEF_EINVAL;
+  const size_t nb = (size_t)grads->K * sizeof(float), tb = nb * grads->layout->L;
+  if (!f32_ok(norms) || !aligned(tensor_norms, 4) || meets_grads(grads, norms, nb))
+    return SAEF_EINVAL;
+  if (tensor_norms != nullptr &&
+      (overlap(norms, nb, tensor_norms, tb) || meets_grads(grads, tensor_norms, tb)))
+    return SAEF_EINVAL;
+  return hip_rc(saef::launch_grad_norm(grads->layout->dev, grads->dev, norm_type == SAEF_NORM_INF,
+                                       norms, tensor_norms, stream));
+}
+
+int saef_clip(const saef_grads* grads, float max_norm, const float* norms, float* out,
+              hipStream_t stream) {
+  if (grads == nullptr) return SAEF_EINVAL;
+  int rc = check_common(grads->layout, grads->K);
+  if (rc != SAEF_OK) return rc;
+  const size_t nb = (size_t)grads->K * sizeof(float);
+  if (!clip_bound_ok(max_norm) || !f32_ok(norms) || !aligned(out, 4)) return SAEF_EINVAL;
+  if (meets_grads(grads, norms, nb)) return SAEF_EINVAL;
+  if (out != nullptr) {
+    const size_t vb = (size_t)grads->K * grads->layout->d_pad * sizeof(float);
+    if (overlap(out, vb, norms, nb) || meets_grads(grads, out, vb)) return SAEF_EINVAL;
+  }
+  return hip_rc(saef::launch_clip(grads->layout->dev, grads->dev, max_norm, norms, out, stream));
 }
 
 int saef_materialize(const saef_layout* layout, int32_t K, int32_t mode, const float* e,
@@ -1236,6 +1382,153 @@ int saef_status(const saef_layout* layout, hipStream_t stream) {
     return SAEF_EHIP;
   if (flag != 0 && hipMemset(layout->dev.status, 0, sizeof(int)) != hipSuccess) return SAEF_EHIP;
   return (flag & saef::kStatusRange) ? SAEF_ERANGE : SAEF_OK;
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- group norm
+
+namespace {
+
+// How the kernels cut a shape: the vector width, the channels of a workgroup
+// and its threads, and the workgroups over the pixels of a sample.
+void cut_group_norm(saef::GroupNormDev& d, int dtype) {
+  const int32_t full = 16 / saef::dtype_bytes(dtype);
+  const int32_t common = std::min(full, d.C & -d.C);
+  d.vec = full;
+  d.threads = saef::kBlock;
+  if (common == full) {
+    d.slab = std::min(d.C, d.threads * full);
+  } else if (d.C / common <= 1024) {
+    // vectors that straddle pixels: the period of their channels is C / common threads
+    d.slab = d.C;
+    if (d.C / common > d.threads) d.threads = 1024;
+  } else {
+    d.vec = 1;
+    d.slab = d.threads;
+  }
+  d.slabs = (d.C + d.slab - 1) / d.slab;
+  // about 8 workgroups for each of the 256 CUs, of at least 4 vectors a thread
+  const int64_t items = (int64_t)d.K * d.N * d.slabs;
+  const int64_t most = d.P * d.slab / ((int64_t)d.threads * d.vec * 4);
+  d.splits = (int32_t)std::max<int64_t>(1, std::min((2048 + items - 1) / items, most));
+}
+
+struct GnSizes {
+  size_t features, params, stats;  // bytes
+};
+GnSizes gn_sizes(const saef_group_norm* p, int64_t ld) {
+  const saef::GroupNormDev& d = p->dev;
+  return {(size_t)d.K * d.N * d.P * d.C * saef::dtype_bytes(p->dtype),
+          ((size_t)(d.K - 1) * ld + d.C) * sizeof(float), (size_t)d.K * d.N * d.G * sizeof(float)};
+}
+
+int check_group_norm(const saef_group_norm* p) {
+  if (p == nullptr) return SAEF_EINVAL;
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess) return SAEF_EHIP;
+  return dev == p->device ? SAEF_OK : SAEF_EINVAL;
+}
+
+}  // namespace
+
+extern "C" {
+
+int saef_group_norm_create(int32_t K, int64_t N, int64_t P, int32_t C, int32_t G, int32_t dtype,
+                           int32_t act, float eps, saef_group_norm** out) {
+  if (out == nullptr) return SAEF_EINVAL;
+  *out = nullptr;
+  if (K < 1 || K > 4096 || N < 1 || P < 1 || C < 1 || C > 65536 || G < 1 || C % G != 0)
+    return SAEF_EINVAL;
+  if (dtype < SAEF_F32 || dtype > SAEF_F16) return SAEF_EINVAL;
+  if (act < SAEF_ACT_NONE || act > SAEF_ACT_SILU) return SAEF_EINVAL;
+  if (!std::isfinite(eps) || !(eps > 0.0f)) return SAEF_EINVAL;
+  const int64_t most = int64_t(1) << 40;  // elements of the features
+  if (N > most / K || P > most / ((int64_t)K * N) || C > most / ((int64_t)K * N * P))
+    return SAEF_EINVAL;
+  saef::GroupNormDev d{};
+  d.K = K;
+  d.N = N;
+  d.P = P;
+  d.C = C;
+  d.G = G;
+  d.Cg = C / G;
+  d.eps = eps;
+  cut_group_norm(d, dtype);
+  // a launch has at most 2^32 - 1 threads
+  if ((double)K * (double)N * d.slabs * d.splits * d.threads >= 4294967296.0) return SAEF_EINVAL;
+  saef_group_norm* p = new (std::nothrow) saef_group_norm();
+  if (p == nullptr) return SAEF_EHIP;
+  p->dtype = dtype;
+  p->act = act;
+  hipError_t err = hipGetDevice(&p->device);
+  if (err == hipSuccess)
+    err = hipMalloc(&p->mem_part, (size_t)K * N * d.splits * C * 2 * sizeof(double));
+  if (err != hipSuccess) {
+    delete p;
+    return SAEF_EHIP;
+  }
+  d.part = static_cast<double*>(p->mem_part);
+  p->dev = d;
+  *out = p;
+  return SAEF_OK;
+}
+
+int saef_group_norm_destroy(saef_group_norm* plan) {
+  if (plan == nullptr) return SAEF_EINVAL;
+  (void)hipFree(plan->mem_part);
+  delete plan;
+  return SAEF_OK;
+}
+
+int saef_group_norm_forward(const saef_group_norm* plan, const void* x, const float* gamma,
+                            const float* beta, int64_t ld, void* y, float* mean, float* rstd,
+                            hipStream_t stream) {
+  int rc = check_group_norm(plan);
+  if (rc != SAEF_OK) return rc;
+  const size_t es = (size_t)saef::dtype_bytes(plan->dtype);
+  if (x == nullptr || y == nullptr || !aligned(x, es) || !aligned(y, es)) return SAEF_EINVAL;
+  if (!f32_ok(gamma) || !f32_ok(beta) || !f32_ok(mean) || !f32_ok(rstd)) return SAEF_EINVAL;
+  if (ld < plan->dev.C || ld > (int64_t(1) << 40)) return SAEF_EINVAL;
+  const GnSizes z = gn_sizes(plan, ld);
+  const Range in[3] = {{x, z.features}, {gamma, z.params}, {beta, z.params}};
+  for (const Range& r : in)
+    if (overlap_any(r.p, r.bytes, {{y, z.features}, {mean, z.stats}, {rstd, z.stats}}))
+      return SAEF_EINVAL;
+  if (overlap_any(y, z.features, {{mean, z.stats}, {rstd, z.stats}}) ||
+      overlap(mean, z.stats, rstd, z.stats))
+    return SAEF_EINVAL;
+  return hip_rc(saef::launch_group_norm_forward(plan->dev, plan->dtype, plan->act, x, gamma, beta,
+                                                ld, y, mean, rstd, stream));
+}
+
+int saef_group_norm_backward(const saef_group_norm* plan, const void* dy, const void* x,
+                             const float* gamma, const float* beta, int64_t ld,
+                             const float* mean, const float* rstd, void* dx, float* dgamma,
+                             float* dbeta, int64_t ldg, hipStream_t stream) {
+  int rc = check_group_norm(plan);
+  if (rc != SAEF_OK) return rc;
+  const size_t es = (size_t)saef::dtype_bytes(plan->dtype);
+  for (const void* p : {dy, x, (const void*)dx})
+    if (p == nullptr || !aligned(p, es)) return SAEF_EINVAL;
+  for (const float* p : {gamma, beta, mean, rstd, (const float*)dgamma, (const float*)dbeta})
+    if (!f32_ok(p)) return SAEF_EINVAL;
+  const int64_t most = int64_t(1) << 40;
+  if (ld < plan->dev.C || ld > most || ldg < plan->dev.C || ldg > most) return SAEF_EINVAL;
+  const GnSizes z = gn_sizes(plan, ld);
+  const size_t gb = gn_sizes(plan, ldg).params;
+  // rows of the two parameters may lie in one another's gaps
+  const size_t row = (size_t)plan->dev.C * sizeof(float);
+  const Range in[6] = {{dy, z.features},  {x, z.features}, {gamma, z.params},
+                       {beta, z.params}, {mean, z.stats}, {rstd, z.stats}};
+  for (const Range& r : in)
+    if (overlap_any(r.p, r.bytes, {{dx, z.features}, {dgamma, gb}, {dbeta, gb}}))
+      return SAEF_EINVAL;
+  if (overlap_any(dx, z.features, {{dgamma, gb}, {dbeta, gb}}) || overlap(dgamma, row, dbeta, row))
+    return SAEF_EINVAL;
+  return hip_rc(saef::launch_group_norm_backward(plan->dev, plan->dtype, plan->act, dy, x, gamma,
+                                                 beta, ld, mean, rstd, dx, dgamma, dbeta, ldg,
+                                                 stream));
 }
 
 }  // extern "C"

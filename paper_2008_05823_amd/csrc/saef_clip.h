@@ -1,0 +1,26 @@
+// Internal declarations of the gradient norm and clipping kernels.
+#pragma once
+
+#include "saef_internal.h"
+
+namespace saef {
+
+// Device-side view of a saef_grads.
+struct GradsDev {
+  void* const* ptr;  // [K L] first element of tensor l of worker k
+  double* part;      // [K n_tiles] partial of each tile
+  double* tpart;     // [K L] the same per tensor
+  int32_t K;
+  int32_t dtype;
+};
+
+// norms[k] = the 2-norm (inf: the largest magnitude) of worker k's gradient;
+// tensor_norms[k][l] alike per tensor when non-null.  Enqueues three kernels.
+hipError_t launch_grad_norm(const DevLayout& lay, const GradsDev& g, bool inf, float* norms,
+                            float* tensor_norms, hipStream_t s);
+
+// out == nullptr: gradients scaled in place; else out[k] (fp32 rows of d_pad).
+hipError_t launch_clip(const DevLayout& lay, const GradsDev& g, float max_norm,
+                       const float* norms, float* out, hipStream_t s);
+
+}  // namespace saef

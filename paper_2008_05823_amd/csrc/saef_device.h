@@ -236,8 +236,43 @@ __device__ __forceinline__ double mean_of(double acc, double inv_k, int K) {
   return (inv_k != 0.0) ? acc * inv_k : acc / (double)K;
 }
 
+// c_k = min(1, max_norm / (norm_k + 1e-6)): the factor that clips a gradient of
+// norm norm_k.  A norm that is no number makes it none.
+__device__ __forceinline__ float clip_factor(float max_norm, float norm) {
+  const float q = max_norm / (norm + 1e-6f);
+  return q >= 1.0f ? 1.0f : q;
+}
+
 // Host: 1/K when K is a power of two (then acc * inv_k == acc / K exactly), else 0.
 inline double inv_pow2(int K) { return (K & (K - 1)) == 0 ? 1.0 / (double)K : 0.0; }
+
+// Elements of the three types in 16-byte vectors of kVec; all arithmetic is in
+// fp32 or wider, rounded to the nearest once when a result is stored.
+template <int kType>
+struct Elem;
+template <>
+struct Elem<kF32> {
+  typedef float T;
+  static constexpr int kVec = 4;
+  static __device__ __forceinline__ float to_f32(T v) { return v; }
+  static __device__ __forceinline__ T of_f32(float v) { return v; }
+};
+template <>
+struct Elem<kBF16> {
+  typedef __bf16 T;
+  static constexpr int kVec = 8;
+  static __device__ __forceinline__ float to_f32(T v) { return (float)v; }
+  static __device__ __forceinline__ T of_f32(float v) { return (T)v; }
+};
+template <>
+struct Elem<kF16> {
+  typedef _Float16 T;
+  static constexpr int kVec = 8;
+  static __device__ __forceinline__ float to_f32(T v) { return (float)v; }
+  static __device__ __forceinline__ T of_f32(float v) { return (T)v; }
+};
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 // The (row, tile) of workgroup b when each tile has `rows` workgroups: along
 // a run, tile by tile, then the next row on the same run.  ti may be past the

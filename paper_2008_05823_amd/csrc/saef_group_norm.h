@@ -1,0 +1,36 @@
+// Internal declarations of the group norm kernels.
+#pragma once
+
+#include "saef_internal.h"
+
+namespace saef {
+
+// Activations (SAEF_ACT_* of the C ABI).
+constexpr int kActNone = 0;
+constexpr int kActRelu = 1;
+constexpr int kActSilu = 2;
+
+// Shape of a group norm over K workers' N samples of P pixels by C channels
+// in G groups, channels last, and how its kernels cut the work.
+struct GroupNormDev {
+  int64_t N, P;
+  int32_t K, C, G, Cg;
+  float eps;
+  int32_t vec;      // elements of a load: 16 bytes' worth, or 1
+  int32_t slab;     // channels of a workgroup: C, or a multiple of vec
+  int32_t slabs;    // ceil(C / slab)
+  int32_t threads;  // of a workgroup; slab divides its active threads' vec elements
+  int32_t splits;   // workgroups over the pixels of a sample
+  double* part;     // [K N splits C 2] sums per channel
+};
+
+hipError_t launch_group_norm_forward(const GroupNormDev& d, int dtype, int act, const void* x,
+                                     const float* gamma, const float* beta, int64_t ld, void* y,
+                                     float* mean, float* rstd, hipStream_t s);
+
+hipError_t launch_group_norm_backward(const GroupNormDev& d, int dtype, int act, const void* dy,
+                                      const void* x, const float* gamma, const float* beta,
+                                      int64_t ld, const float* mean, const float* rstd, void* dx,
+                                      float* dgamma, float* dbeta, int64_t ldg, hipStream_t s);
+
+}  // namespace saef

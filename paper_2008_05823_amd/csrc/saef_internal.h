@@ -72,6 +72,12 @@ struct DevLayout {
   int32_t k_max;
 };
 
+// Element types of gradients and features (SAEF_F32, SAEF_BF16, SAEF_F16 of the C ABI).
+constexpr int kF32 = 0;
+constexpr int kBF16 = 1;
+constexpr int kF16 = 2;
+constexpr int dtype_bytes(int dtype) { return dtype == kF32 ? 4 : 2; }
+
 // status flag bits
 constexpr int kStatusRange = 1;
 
@@ -91,10 +97,12 @@ struct LaunchEvents {
 // non-null: momentum, m <- fma(mu, m, g) and Delta = fma(lr, m, e); else
 // Delta = fma(lr, g, e).  Always writes Delta (before correction) into e,
 // the new sign words and the tile partial sums; launch_finalize then writes
-// the new scales.
+// the new scales.  norms non-null: g[k] scaled by min(1, max_norm / (norms[k] +
+// 1e-6)) on read.
 hipError_t launch_compress(const DevLayout& lay, int K, float lr, float mu, const float* g,
                            float* m, float* e, uint64_t* signs, const float* scales, bool decode,
-                           hipStream_t s, const LaunchEvents& ev = LaunchEvents());
+                           hipStream_t s, const LaunchEvents& ev = LaunchEvents(),
+                           float max_norm = 0.0f, const float* norms = nullptr);
 
 // Step ahead and worker compression in one pass (the gradient is in place
 // before the step ahead): launch_step_ahead's xh without averaging, then

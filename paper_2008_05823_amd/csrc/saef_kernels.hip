@@ -210,10 +210,11 @@ constexpr int kXhDec = 2;
 // fma(lr, m or g, e) (e decoded when kDecode), sign words by ballot,
 // exact-sum terms, Delta stored.  kXh: the step ahead xh = x - e from the
 // same read of e (sx: the server's sign words of the tile).  kFull: all kN
-// words are whole words of the tile (no lane masks).
-template <bool kDecode, bool kMom, int kXh, bool kFull, int kN>
+// words are whole words of the tile (no lane masks).  kClip: the gradient is
+// scaled by `clip` as it is read.
+template <bool kDecode, bool kMom, int kXh, bool kClip, bool kFull, int kN>
 __device__ __forceinline__ void compress_words(int w0, int nw, int count, float lr, float mu,
-                                               Buf rg, Buf rm, Buf re, Buf rs, Buf rx, Buf rh,
+                                               float clip, Buf rg, Buf rm, Buf re, Buf rs, Buf rx, Buf rh,
                                                const uint64_t* __restrict__ sx, const Corr& c_old,
                                                const Corr& c_x, ExactSum& acc) {
   const int lane = lane_id();
@@ -247,8 +248,9 @@ __device__ __forceinline__ void compress_words(int w0, int nw, int count, float 
       buf_st(rh, off, xc - ev2);                // x^(k)_{t+1/2} = x_t - e^(k)_t
     }
     float step = gv[u];
+    if (kClip) step = clip * step;
     if (kMom) {
-      step = __builtin_fmaf(mu, mv[u], gv[u]);  // m^(k)_{t+1} = mu m^(k)_t + grad
+      step = __builtin_fmaf(mu, mv[u], step);  // m^(k)_{t+1} = mu m^(k)_t + grad
       buf_st(rm, off, step);
     }
     // Delta^(k) = e^(k) + lr * m^(k)_{t+1}, one rounding (m = grad when mu = 0)
@@ -270,9 +272,9 @@ __device__ __forceinline__ void compress_words(int w0, int nw, int count, float 
 
 // Worker k's tile ti by a workgroup of kNW waves of kN words per pass: wave
 // w takes words w*kN .. w*kN+kN-1, then strides by kNW*kN words.
-template <bool kDecode, bool kMom, int kXh, int kNW, int kN>
+template <bool kDecode, bool kMom, int kXh, bool kClip, int kNW, int kN>
 __device__ __forceinline__ void compress_tile(const DevLayout& lay, int k, int64_t ti, float lr,
-                                              float mu, const float* __restrict__ g,
+                                              float mu, float clip, const float* __restrict__ g,
                                               float* __restrict__ m, float* __restrict__ e,
                                               uint64_t* __restrict__ signs,
                                               const float* __restrict__ scales,
@@ -299,11 +301,12 @@ __device__ __forceinline__ void compress_tile(const DevLayout& lay, int k, int64
   ExactSum acc;
   for (int w0 = wave * kN; w0 < nw; w0 += kNW * kN) {
     if ((w0 + kN) * 64 <= tile.count) {
-      compress_words<kDecode, kMom, kXh, true, kN>(w0, nw, tile.count, lr, mu, rg, rm, re, rs, rx,
-                                                   rh, sx, c_old, c_x, acc);
+      compress_words<kDecode, kMom, kXh, kClip, true, kN>(w0, nw, tile.count, lr, mu, clip, rg, rm,
+                                                          re, rs, rx, rh, sx, c_old, c_x, acc);
     } else {
-      compress_words<kDecode, kMom, kXh, false, kN>(w0, nw, tile.count, lr, mu, rg, rm, re, rs,
-                                                    rx, rh, sx, c_old, c_x, acc);
+      compress_words<kDecode, kMom, kXh, kClip, false, kN>(w0, nw, tile.count, lr, mu, clip, rg,
+                                                           rm, re, rs, rx, rh, sx, c_old, c_x,
+                                                           acc);
     }
     acc.added(kN);
   }
@@ -327,9 +330,9 @@ k_compress(DevLayout lay, int K, float lr, float mu, const float* __restrict__ g
            float* __restrict__ m, float* __restrict__ e, uint64_t* __restrict__ signs,
            const float* __restrict__ scales) {
   const unsigned b = blockIdx.x;
-  compress_tile<kDecode, false, kXhNone, kSWaves, kU>(lay, (int)(b % (unsigned)K),
-                                                      b / (unsigned)K, lr, mu, g, m, e, signs,
-                                                      scales, nullptr, nullptr, nullptr, nullptr);
+  compress_tile<kDecode, false, kXhNone, false, kSWaves, kU>(
+      lay, (int)(b % (unsigned)K), b / (unsigned)K, lr, mu, 1.0f, g, m, e, signs, scales, nullptr,
+      nullptr, nullptr, nullptr);
 }
 
 // With momentum (three streams in, two out): 665 us at 4 waves per SIMD, 674
@@ -340,9 +343,26 @@ k_compress_mom(DevLayout lay, int K, float lr, float mu, const float* __restrict
                float* __restrict__ m, float* __restrict__ e, uint64_t* __restrict__ signs,
                const float* __restrict__ scales) {
   const unsigned b = blockIdx.x;
-  compress_tile<kDecode, true, kXhNone, kSWaves, kU>(lay, (int)(b % (unsigned)K),
-                                                     b / (unsigned)K, lr, mu, g, m, e, signs,
-                                                     scales, nullptr, nullptr, nullptr, nullptr);
+  compress_tile<kDecode, true, kXhNone, false, kSWaves, kU>(
+      lay, (int)(b % (unsigned)K), b / (unsigned)K, lr, mu, 1.0f, g, m, e, signs, scales, nullptr,
+      nullptr, nullptr, nullptr);
+}
+
+// The two on gradients clipped as they are read: worker k's by clip_factor of
+// its norm, one factor and one rounding an element, instead of a pass of its own
+// over the gradients (8 bytes an element).
+template <bool kDecode, bool kMom>
+__global__ __launch_bounds__(kSBlock) __attribute__((
+    amdgpu_waves_per_eu(1, kDecode && !kMom ? 8 : 4))) void
+k_compress_clipped(DevLayout lay, int K, float lr, float mu, float max_norm,
+                   const float* __restrict__ norms, const float* __restrict__ g,
+                   float* __restrict__ m, float* __restrict__ e, uint64_t* __restrict__ signs,
+                   const float* __restrict__ scales) {
+  const unsigned b = blockIdx.x;
+  const int k = (int)(b % (unsigned)K);
+  compress_tile<kDecode, kMom, kXhNone, true, kSWaves, kU>(
+      lay, k, b / (unsigned)K, lr, mu, clip_factor(max_norm, norms[k]), g, m, e, signs, scales,
+      nullptr, nullptr, nullptr, nullptr);
 }
 
 // ------------------------------------------------------------------ worker step
@@ -370,8 +390,8 @@ k_worker(DevLayout lay, int K, float lr, float mu, const float* __restrict__ g,
   int64_t ti;
   run_tile_of(blockIdx.x, K, tile_run_shift(lay.n_tiles), k, ti);
   if (ti >= lay.n_tiles) return;
-  compress_tile<kDecode, kMom, kXh, kWWaves, kWU>(lay, k, ti, lr, mu, g, m, e, signs, scales, x,
-                                                  ss, sscales, xh);
+  compress_tile<kDecode, kMom, kXh, false, kWWaves, kWU>(lay, k, ti, lr, mu, 1.0f, g, m, e, signs,
+                                                         scales, x, ss, sscales, xh);
 }
 
 // ------------------------------------------------------------------ finalize
@@ -1239,8 +1259,21 @@ hipError_t launch_stream_probe(const float* a, const float* b, float* c, int64_t
 
 hipError_t launch_compress(const DevLayout& lay, int K, float lr, float mu, const float* g,
                            float* m, float* e, uint64_t* signs, const float* scales, bool decode,
-                           hipStream_t s, const LaunchEvents& ev) {
+                           hipStream_t s, const LaunchEvents& ev, float max_norm,
+                           const float* norms) {
   const dim3 grid((unsigned)(lay.n_tiles * K));
+  if (norms != nullptr) {
+#define SAEF_CMP_CL(D, M)                                                                       \
+  SAEF_LAUNCH((k_compress_clipped<D, M>), grid, dim3(kSBlock), 0, s, lay, K, lr, mu, max_norm, \
+              norms, g, m, e, signs, scales)
+    if (m != nullptr) {
+      if (decode) SAEF_CMP_CL(true, true); else SAEF_CMP_CL(false, true);
+    } else {
+      if (decode) SAEF_CMP_CL(true, false); else SAEF_CMP_CL(false, false);
+    }
+#undef SAEF_CMP_CL
+    return hipGetLastError();
+  }
 #define SAEF_CMP(KERNEL, D) \
   SAEF_LAUNCH((KERNEL<D>), grid, dim3(kSBlock), 0, s, lay, K, lr, mu, g, m, e, signs, scales)
   if (m != nullptr) {

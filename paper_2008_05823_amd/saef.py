@@ -11,6 +11,7 @@ not been built (``python -c "import __graft_entry__ as g; g.build()"``).
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import torch
@@ -22,6 +23,8 @@ LIB_PATH = os.environ.get("SAEF_LIBRARY") or os.path.join(HERE, "libsaef.so")
 OK, EINVAL, ERANGE, EHIP = 0, -1, -2, -3
 MODE_SC, MODE_DC = 0, 1
 VARIANT_EF, VARIANT_SAEF = 0, 1
+NORM_2, NORM_INF = 0, 1
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build the HIP library first "
@@ -50,6 +53,17 @@ _SIGS = {
                          _P],
     "saef_round_end": [_P, _i64, _i64, _i32, _f32, _f32, _i32, _P, _P, _P, _P, _P, _P, _P, _P,
                        _P, _P],
+    "saef_round_end_clipped": [_P, _i64, _i64, _i32, _f32, _f32, _i32, _f32, _P, _P, _P, _P, _P, _P,
+                               _P, _P, _P, _P, _P],
+    "saef_group_norm_create": [_i32, _i64, _i64, _i32, _i32, _i32, _i32, _f32,
+                               ctypes.POINTER(_P)],
+    "saef_group_norm_destroy": [_P],
+    "saef_group_norm_forward": [_P, _P, _P, _P, _i64, _P, _P, _P, _P],
+    "saef_group_norm_backward": [_P, _P, _P, _P, _P, _i64, _P, _P, _P, _P, _P, _i64, _P],
+    "saef_grads_create": [_P, _i32, _i32, _P, ctypes.POINTER(_P)],
+    "saef_grads_destroy": [_P],
+    "saef_grad_norm": [_P, _i32, _P, _P, _P],
+    "saef_clip": [_P, _f32, _P, _P, _P],
     "saef_topk_create": [_P, _P, ctypes.POINTER(_P)],
     "saef_topk_destroy": [_P],
     "saef_topk_info": [_P, _P],
@@ -137,6 +151,8 @@ class Layout:
         self.L = len(off)
         self.d_pad = int(d_pad)
         self.k_max = int(k_max)
+        self.offsets = [int(v) for v in off]
+        self.sizes = [int(v) for v in n]
 
     @property
     def handle(self):
@@ -221,6 +237,193 @@ def saef_round_momentum(layout: Layout, t: int, period: int, K: int, lr: float, 
            _lib.saef_round_momentum(layout.handle, t, period, K, lr, mu, mode, _f(g), _f(m),
                                     _f(e), _f(e_srv), _f(x), _f(xh), _w(signs), _f(scales),
                                     _w(srv_signs), _f(srv_scales), _stream(stream)))
+
+
+# element types of gradients and features (SAEF_F32, SAEF_BF16, SAEF_F16)
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+class Grads:
+    """Where K workers' gradients lie (see saef_grads_create).  src: the rows of
+    a (K, d_pad) tensor, or one sequence per worker of its L tensors in layout
+    order (any shapes of n[l] elements, contiguous); fp32, bf16 or fp16
+    throughout.  The tensors are kept alive."""
+
+    def __init__(self, layout: "Layout", src):
+        if isinstance(src, torch.Tensor):
+            if src.dim() != 2 or src.shape[1] != layout.d_pad:
+                raise ValueError("gradient rows must be (K, d_pad)")
+            dtype, K = src.dtype, src.shape[0]
+            base = _dev(src, dtype)
+            es = src.element_size()
+            ptrs = [base + (k * layout.d_pad + o) * es for k in range(K) for o in layout.offsets]
+            self.tensors = [src]
+        else:
+            rows = [list(r) for r in src]
+            if not rows or any(len(r) != layout.L for r in rows):
+                raise ValueError("one gradient per worker and tensor")
+            dtype, K = rows[0][0].dtype, len(rows)
+            for r in rows:
+                if [v.numel() for v in r] != layout.sizes:
+                    raise ValueError("a gradient's size differs from its tensor's")
+            ptrs = [_dev(v, dtype) for r in rows for v in r]
+            self.tensors = [v for r in rows for v in r]
+        if dtype not in DTYPES:
+            raise TypeError(f"gradients must be float32, bfloat16 or float16, got {dtype}")
+        table = (_P * len(ptrs))(*ptrs)
+        handle = _P()
+        _check("saef_grads_create", _lib.saef_grads_create(layout.handle, K, DTYPES[dtype], table,
+                                                           ctypes.byref(handle)))
+        self._h = handle
+        self.layout = layout  # the layout must outlive the handle
+        self.K = K
+        self.dtype = dtype
+
+    @property
+    def handle(self):
+        if self._h is None:
+            raise ValueError("gradients destroyed")
+        return self._h
+
+    def destroy(self):
+        if getattr(self, "_h", None) is not None:
+            _check("saef_grads_destroy", _lib.saef_grads_destroy(self._h))
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def _sized(t, n, what):
+    if t is not None and t.numel() != n:
+        raise ValueError(f"{what} must have {n} elements, got {t.numel()}")
+    return t
+
+
+def saef_grad_norm(grads: Grads, norms, tensor_norms=None, norm_type=2, stream=None):
+    """Each worker's gradient norm into norms (K) and, per tensor, into
+    tensor_norms (K, L); norm_type 2 or math.inf."""
+    kinds = {2: NORM_2, math.inf: NORM_INF}
+    if norm_type not in kinds:
+        raise ValueError(f"norm_type must be 2 or inf, got {norm_type!r}")
+    _sized(norms, grads.K, "norms")
+    _sized(tensor_norms, grads.K * grads.layout.L, "tensor_norms")
+    _check("saef_grad_norm",
+           _lib.saef_grad_norm(grads.handle, kinds[norm_type], _f(norms), _f(tensor_norms),
+                               _stream(stream)))
+
+
+def saef_clip(grads: Grads, max_norm: float, norms, out=None, stream=None):
+    """Gradients scaled to at most max_norm: into the fp32 rows out (K, d_pad),
+    or in place (out None)."""
+    _sized(norms, grads.K, "norms")
+    _sized(out, grads.K * grads.layout.d_pad, "out")
+    _check("saef_clip", _lib.saef_clip(grads.handle, max_norm, _f(norms), _f(out),
+                                       _stream(stream)))
+
+
+def saef_round_end_clipped(layout: Layout, t: int, period: int, K: int, lr: float, mu: float,
+                           mode: int, max_norm: float, norms, g, m, e, e_srv, x, signs, scales,
+                           srv_signs=None, srv_scales=None, stream=None):
+    """Second half of iteration t on gradients clipped to max_norm as they are read."""
+    _sized(norms, K, "norms")
+    _check("saef_round_end_clipped",
+           _lib.saef_round_end_clipped(layout.handle, t, period, K, lr, mu, mode, max_norm,
+                                       _f(norms), _f(g), _f(m), _f(e), _f(e_srv), _f(x),
+                                       _w(signs), _f(scales), _w(srv_signs), _f(srv_scales),
+                                       _stream(stream)))
+
+
+class GroupNorm:
+    """A group norm over K workers' N samples of P pixels by C channels in G
+    groups, channels last, with an activation (see saef_group_norm_create)."""
+
+    def __init__(self, K: int, N: int, P: int, C: int, G: int, dtype=torch.float32,
+                 act: int = ACT_NONE, eps: float = 1e-5):
+        if dtype not in DTYPES:
+            raise TypeError(f"features must be float32, bfloat16 or float16, got {dtype}")
+        handle = _P()
+        _check("saef_group_norm_create",
+               _lib.saef_group_norm_create(K, N, P, C, G, DTYPES[dtype], act, eps,
+                                           ctypes.byref(handle)))
+        self._h = handle
+        self.K, self.N, self.P, self.C, self.G = K, N, P, C, G
+        self.dtype = dtype
+
+    @property
+    def handle(self):
+        if self._h is None:
+            raise ValueError("group norm destroyed")
+        return self._h
+
+    def _features(self, t, what):
+        """Address of K N P C features: a contiguous tensor whose last dimension is
+        C, or (K N, C, H, W) in torch's channels_last memory format."""
+        _sized(t, self.K * self.N * self.P * self.C, what)
+        if t.dim() == 4 and t.shape[:2] == (self.K * self.N, self.C) \
+                and t.is_contiguous(memory_format=torch.channels_last):
+            t = t.permute(0, 2, 3, 1)
+        if t.shape[-1:] != (self.C,):
+            raise ValueError(f"{what} must be channels last, C = {self.C}")
+        return _dev(t, self.dtype)
+
+    def _params(self, t, what):
+        """Address and worker stride of (K, C) values, contiguous along C."""
+        if tuple(t.shape) != (self.K, self.C):
+            raise ValueError(f"{what} must be (K, C) = {(self.K, self.C)}, got {tuple(t.shape)}")
+        if not t.is_cuda:
+            raise TypeError("SAEF buffers must be device tensors")
+        if t.dtype != torch.float32:
+            raise TypeError(f"expected {torch.float32}, got {t.dtype}")
+        if self.C > 1 and t.stride(1) != 1:
+            raise ValueError(f"{what} must be contiguous along C")
+        return t.data_ptr(), t.stride(0) if self.K > 1 else self.C
+
+    def _pair(self, a, b, what):
+        (pa, la), (pb, lb) = self._params(a, what[0]), self._params(b, what[1])
+        if la != lb:
+            raise ValueError(f"{what[0]} and {what[1]} must have the same worker stride")
+        return pa, pb, la
+
+    def destroy(self):
+        if getattr(self, "_h", None) is not None:
+            _check("saef_group_norm_destroy", _lib.saef_group_norm_destroy(self._h))
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def saef_group_norm_forward(plan: GroupNorm, x, gamma, beta, y, mean, rstd, stream=None):
+    """y = act(gamma (x - mean) rstd + beta); gamma, beta (K, C), e.g. columns
+    of the evaluation points xh; mean, rstd (K, N, G) are written."""
+    pg, pb, ld = plan._pair(gamma, beta, ("gamma", "beta"))
+    for t, what in ((mean, "mean"), (rstd, "rstd")):
+        _sized(t, plan.K * plan.N * plan.G, what)
+    _check("saef_group_norm_forward",
+           _lib.saef_group_norm_forward(plan.handle, plan._features(x, "x"), pg, pb, ld,
+                                        plan._features(y, "y"), _f(mean), _f(rstd),
+                                        _stream(stream)))
+
+
+def saef_group_norm_backward(plan: GroupNorm, dy, x, gamma, beta, mean, rstd, dx, dgamma, dbeta,
+                             stream=None):
+    """dx, and dgamma, dbeta (K, C), e.g. columns of the gradient rows g."""
+    pg, pb, ld = plan._pair(gamma, beta, ("gamma", "beta"))
+    qg, qb, ldg = plan._pair(dgamma, dbeta, ("dgamma", "dbeta"))
+    for t, what in ((mean, "mean"), (rstd, "rstd")):
+        _sized(t, plan.K * plan.N * plan.G, what)
+    _check("saef_group_norm_backward",
+           _lib.saef_group_norm_backward(plan.handle, plan._features(dy, "dy"),
+                                         plan._features(x, "x"), pg, pb, ld, _f(mean), _f(rstd),
+                                         plan._features(dx, "dx"), qg, qb, ldg,
+                                         _stream(stream)))
 
 
 def _u32(t):
