@@ -86,7 +86,7 @@ struct saef_grads {
   saef::GradsDev dev{};
   void* mem_ptr = nullptr;
   void* mem_part = nullptr;
-  void* mem_tpart = nullptr;
+  void* mem_runs = nullptr;
 };
 
 // The shape of a group norm and the scratch of its sums.
@@ -95,7 +95,9 @@ struct saef_group_norm {
   int32_t dtype = 0;
   int32_t act = 0;
   saef::GroupNormDev dev{};
+  saef::GroupNormHeld fwd{}, bwd{};
   void* mem_part = nullptr;
+  void* mem_pieces = nullptr;
 };
 
 namespace {
@@ -781,7 +783,13 @@ int saef_grads_create(const saef_layout* layout, int32_t K, int32_t dtype, void*
   hipError_t err = hipMalloc(&g->mem_ptr, rows * sizeof(void*));
   if (err == hipSuccess)
     err = hipMalloc(&g->mem_part, (size_t)K * layout->dev.n_tiles * sizeof(double));
-  if (err == hipSuccess) err = hipMalloc(&g->mem_tpart, rows * sizeof(double));
+  const int64_t pairs = layout->dev.n_tiles * K;
+  int32_t run_tiles = 1;
+  while (run_tiles < 32 && pairs / run_tiles > 32768) run_tiles *= 2;
+  const int64_t runs = (layout->dev.n_tiles + run_tiles - 1) / run_tiles;
+  // What is read for the norm is read again to be clipped
+  const int32_t cached = (double)K * layout->d_pad * es <= 1073741824.0;
+  if (err == hipSuccess) err = hipMalloc(&g->mem_runs, (size_t)K * runs * sizeof(double));
   if (err == hipSuccess)
     err = hipMemcpy(g->mem_ptr, ptr, rows * sizeof(void*), hipMemcpyHostToDevice);
   if (err != hipSuccess) {
@@ -789,14 +797,14 @@ int saef_grads_create(const saef_layout* layout, int32_t K, int32_t dtype, void*
     return SAEF_EHIP;
   }
   g->dev = saef::GradsDev{static_cast<void* const*>(g->mem_ptr), static_cast<double*>(g->mem_part),
-                          static_cast<double*>(g->mem_tpart), K, dtype};
+                          static_cast<double*>(g->mem_runs), runs, run_tiles, cached, K, dtype};
   *out = g;
   return SAEF_OK;
 }
 
 int saef_grads_destroy(saef_grads* grads) {
   if (grads == nullptr) return SAEF_EINVAL;
-  for (void* q : {grads->mem_ptr, grads->mem_part, grads->mem_tpart}) (void)hipFree(q);
+  for (void* q : {grads->mem_ptr, grads->mem_part, grads->mem_runs}) (void)hipFree(q);
   delete grads;
   return SAEF_OK;
 }
@@ -1390,28 +1398,60 @@ int saef_status(const saef_layout* layout, hipStream_t stream) {
 
 namespace {
 
-// How the kernels cut a shape: the vector width, the channels of a workgroup
-// and its threads, and the workgroups over the pixels of a sample.
+// How the kernels that read the features twice cut a shape: the vector width, the
+// channels of a workgroup and the workgroups over the pixels of a sample.
 void cut_group_norm(saef::GroupNormDev& d, int dtype) {
   const int32_t full = 16 / saef::dtype_bytes(dtype);
   const int32_t common = std::min(full, d.C & -d.C);
   d.vec = full;
-  d.threads = saef::kBlock;
   if (common == full) {
-    d.slab = std::min(d.C, d.threads * full);
-  } else if (d.C / common <= 1024) {
+    // rows of 512 bytes, of whole groups where that is no more than twice as long
+    const int32_t unit = d.Cg / std::min(full, d.Cg & -d.Cg) * full, row = 32 * full;
+    d.slab = std::min(d.C, unit <= 2 * row ? (row + unit - 1) / unit * unit : row);
+  } else if (d.C / common <= saef::kBlock) {
     // vectors that straddle pixels: the period of their channels is C / common threads
     d.slab = d.C;
-    if (d.C / common > d.threads) d.threads = 1024;
   } else {
     d.vec = 1;
-    d.slab = d.threads;
+    d.slab = saef::kBlock;
   }
   d.slabs = (d.C + d.slab - 1) / d.slab;
-  // about 8 workgroups for each of the 256 CUs, of at least 4 vectors a thread
-  const int64_t items = (int64_t)d.K * d.N * d.slabs;
-  const int64_t most = d.P * d.slab / ((int64_t)d.threads * d.vec * 4);
-  d.splits = (int32_t)std::max<int64_t>(1, std::min((2048 + items - 1) / items, most));
+  // About 2 workgroups for each of the 256 CUs (more make the second pass join more
+  // sums: 50 MB forward 20.6 us, 24 with 4), of at least 8 vectors a thread, and at most
+  // 64 (the backward sums add a thread's values in fp32).
+  const int64_t wgs = 512;
+  const int64_t items = (int64_t)d.K * d.N * d.slabs, round = (int64_t)saef::kBlock * d.vec;
+  const int64_t most = d.P * d.slab / (round * 8), least = d.P * d.slab / (round * 64) + 1;
+  d.splits = (int32_t)std::max(least, std::min((wgs + items - 1) / items, most));
+  d.backwards = (double)d.K * d.N * d.P * d.C * saef::dtype_bytes(dtype) > 268435456.0;
+}
+
+// Whether, and how, features are held in registers between the sums and the
+// result.
+saef::GroupNormHeld hold_group_norm(const saef::GroupNormDev& d, int dtype, bool back) {
+  const int32_t es = saef::dtype_bytes(dtype), vec = 16 / es;
+  const saef::GroupNormHeld none{0, 0, 0, 0};
+  if (d.C % vec != 0 || d.P > (int64_t(1) << 31) / es / d.C - 1) return none;
+  const int32_t unit = d.Cg / std::min(vec, d.Cg & -d.Cg) * vec;  // whole groups and vectors
+  const bool one = d.Cg % vec == 0;
+  // Small workgroups first, then long rows; rows of less than 128 bytes only where
+  // there are no more channels.
+  for (int32_t most : {256, 512})
+    for (int32_t row : {256, 128}) {
+      int32_t slab = std::min(d.C, (row / es + unit - 1) / unit * unit);
+      // a pixel or few: wider slabs
+      while (slab < d.C && d.P * slab < 512 * vec) slab = std::min(d.C, 2 * slab);
+      const int32_t cols = slab / vec;
+      for (int32_t vectors : {2, 4, 8, 16}) {
+        if (vectors == 16 && back) continue;  // (their values do not fit the registers)
+        const int64_t threads = ((d.P + vectors - 1) / vectors * cols + 63) / 64 * 64;
+        const size_t lds = back ? (size_t)threads * vec * 8 + (size_t)slab * 24
+                                : (size_t)threads * (one ? 1 : vec) * 16 + (size_t)slab * 12;
+        if (threads > most || lds > 65536) continue;
+        return {(int32_t)threads, vectors, slab, (d.C + slab - 1) / slab};
+      }
+    }
+  return none;
 }
 
 struct GnSizes {
@@ -1455,20 +1495,30 @@ int saef_group_norm_create(int32_t K, int64_t N, int64_t P, int32_t C, int32_t G
   d.Cg = C / G;
   d.eps = eps;
   cut_group_norm(d, dtype);
+  const saef::GroupNormHeld fwd = hold_group_norm(d, dtype, false);
+  const saef::GroupNormHeld bwd = hold_group_norm(d, dtype, true);
   // a launch has at most 2^32 - 1 threads
-  if ((double)K * (double)N * d.slabs * d.splits * d.threads >= 4294967296.0) return SAEF_EINVAL;
+  const double items = (double)K * (double)N;
+  if (items * d.slabs * d.splits * saef::kBlock >= 4294967296.0 ||
+      items * fwd.slabs * fwd.threads >= 4294967296.0 ||
+      items * bwd.slabs * bwd.threads >= 4294967296.0)
+    return SAEF_EINVAL;
   saef_group_norm* p = new (std::nothrow) saef_group_norm();
   if (p == nullptr) return SAEF_EHIP;
   p->dtype = dtype;
   p->act = act;
+  p->fwd = fwd;
+  p->bwd = bwd;
   hipError_t err = hipGetDevice(&p->device);
-  if (err == hipSuccess)
-    err = hipMalloc(&p->mem_part, (size_t)K * N * d.splits * C * 2 * sizeof(double));
+  const size_t rows = (size_t)K * N * d.splits, pair = 2 * sizeof(double);
+  if (err == hipSuccess) err = hipMalloc(&p->mem_part, rows * C * pair);
+  if (err == hipSuccess) err = hipMalloc(&p->mem_pieces, rows * (G + d.slabs - 1) * pair);
   if (err != hipSuccess) {
-    delete p;
+    (void)saef_group_norm_destroy(p);
     return SAEF_EHIP;
   }
   d.part = static_cast<double*>(p->mem_part);
+  d.pieces = static_cast<double*>(p->mem_pieces);
   p->dev = d;
   *out = p;
   return SAEF_OK;
@@ -1477,6 +1527,7 @@ int saef_group_norm_create(int32_t K, int64_t N, int64_t P, int32_t C, int32_t G
 int saef_group_norm_destroy(saef_group_norm* plan) {
   if (plan == nullptr) return SAEF_EINVAL;
   (void)hipFree(plan->mem_part);
+  (void)hipFree(plan->mem_pieces);
   delete plan;
   return SAEF_OK;
 }
@@ -1498,8 +1549,8 @@ int saef_group_norm_forward(const saef_group_norm* plan, const void* x, const fl
   if (overlap_any(y, z.features, {{mean, z.stats}, {rstd, z.stats}}) ||
       overlap(mean, z.stats, rstd, z.stats))
     return SAEF_EINVAL;
-  return hip_rc(saef::launch_group_norm_forward(plan->dev, plan->dtype, plan->act, x, gamma, beta,
-                                                ld, y, mean, rstd, stream));
+  return hip_rc(saef::launch_group_norm_forward(plan->dev, plan->fwd, plan->dtype, plan->act, x,
+                                                gamma, beta, ld, y, mean, rstd, stream));
 }
 
 int saef_group_norm_backward(const saef_group_norm* plan, const void* dy, const void* x,
@@ -1526,9 +1577,9 @@ int saef_group_norm_backward(const saef_group_norm* plan, const void* dy, const 
       return SAEF_EINVAL;
   if (overlap_any(dx, z.features, {{dgamma, gb}, {dbeta, gb}}) || overlap(dgamma, row, dbeta, row))
     return SAEF_EINVAL;
-  return hip_rc(saef::launch_group_norm_backward(plan->dev, plan->dtype, plan->act, dy, x, gamma,
-                                                 beta, ld, mean, rstd, dx, dgamma, dbeta, ldg,
-                                                 stream));
+  return hip_rc(saef::launch_group_norm_backward(plan->dev, plan->bwd, plan->dtype, plan->act, dy,
+                                                 x, gamma, beta, ld, mean, rstd, dx, dgamma,
+                                                 dbeta, ldg, stream));
 }
 
 }  // extern "C"

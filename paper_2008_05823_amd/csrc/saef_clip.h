@@ -8,14 +8,17 @@ namespace saef {
 // Device-side view of a saef_grads.
 struct GradsDev {
   void* const* ptr;  // [K L] first element of tensor l of worker k
-  double* part;      // [K n_tiles] partial of each tile
-  double* tpart;     // [K L] the same per tensor
+  double* part;      // [K n_tiles] a tensor's part of a run, at its first tile there
+  double* run_sums;  // [K runs] sum of each run
+  int64_t runs;      // runs of run_tiles tiles, a wave each
+  int32_t run_tiles;
+  int32_t cached;    // the norm's loads stay in the last-level cache
   int32_t K;
   int32_t dtype;
 };
 
 // norms[k] = the 2-norm (inf: the largest magnitude) of worker k's gradient;
-// tensor_norms[k][l] alike per tensor when non-null.  Enqueues three kernels.
+// tensor_norms[k][l] alike per tensor when non-null.  Enqueues two kernels.
 hipError_t launch_grad_norm(const DevLayout& lay, const GradsDev& g, bool inf, float* norms,
                             float* tensor_norms, hipStream_t s);
 

@@ -53,7 +53,12 @@ struct Acc {
       s = __builtin_fma((double)v, (double)v, s);
     }
   }
-  __device__ __forceinline__ double wave() {
+  __device__ __forceinline__ void join(const Acc& o) {
+    s += o.s;
+    m = max(m, o.m);
+  }
+  __device__ __forceinline__ double wave() const { return Acc(*this).fold(); }
+  __device__ __forceinline__ double fold() {
     if (kInf) {
 #pragma unroll
       for (int o = kWave / 2; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
@@ -65,53 +70,87 @@ struct Acc {
   }
 };
 
+constexpr int kFinWaves = 4;  // of a workgroup that joins sums
+
 constexpr int kGU = 8;  // 16-byte loads of a wave in flight
 
-// Grid: K runs of ceil(n_tiles / 4) workgroups, a wave per (worker, tile).
-template <int kType, bool kInf>
-__global__ __launch_bounds__(kBlock) void k_grad_tiles(DevLayout lay, GradsDev g) {
-  const unsigned per = (unsigned)((lay.n_tiles + kWaves - 1) / kWaves);
-  const int k = (int)(blockIdx.x / per);
-  const int64_t ti = (int64_t)(blockIdx.x % per) * kWaves + wave_id();
-  if (ti >= lay.n_tiles) return;
-  const int lane = lane_id();
-  const Span<kType> sp(lay, g, k, lay.tiles[ti]);
-  typedef Elem<kType> E;
-  const Buf b = sp.body();
-  Acc<kInf> acc;
-  for (int v0 = 0; v0 < sp.nvec; v0 += kGU * kWave) {
-    u32x4 raw[kGU];
-#pragma unroll
-    for (int u = 0; u < kGU; ++u)
-      raw[u] = __builtin_amdgcn_raw_buffer_load_b128(b, (v0 + u * kWave + lane) * 16, 0, kAuxNT);
-#pragma unroll
-    for (int u = 0; u < kGU; ++u) {
-      typename E::T v[E::kVec];
-      __builtin_memcpy(v, &raw[u], 16);
-#pragma unroll
-      for (int j = 0; j < E::kVec; ++j) acc.add(E::to_f32(v[j]));
-    }
+// The run of tiles [first, last) and the worker of this wave.  Grid: K times
+// ceil(runs / 4) workgroups, worker by worker, a wave per run.
+struct Run {
+  int k;
+  int64_t run, first, last;
+  __device__ __forceinline__ Run(const DevLayout& lay, const GradsDev& g, unsigned block) {
+    const unsigned per = (unsigned)((g.runs + kWaves - 1) / kWaves);
+    k = (int)(block / per);
+    run = (int64_t)(block % per) * kWaves + wave_id();
+    first = run * g.run_tiles;
+    last = min(first + g.run_tiles, lay.n_tiles);
   }
-  if (lane < sp.head) acc.add(E::to_f32(sp.p[lane]));
-  if (lane < sp.tail) acc.add(E::to_f32(sp.tail_at()[lane]));
-  const double s = acc.wave();
-  if (lane == 0) g.part[(int64_t)k * lay.n_tiles + ti] = s;
+};
+
+// A wave adds up its run tile by tile.  The run's sum goes to runs[k][run]; where
+// tensor sums are asked for, the part of each tensor in the run goes to the slot
+// of its first tile there.
+template <int kType, bool kInf, bool kTensors, int kAux>
+__global__ __launch_bounds__(kBlock) void k_grad_tiles(DevLayout lay, GradsDev g) {
+  const Run r(lay, g, blockIdx.x);
+  if (r.first >= lay.n_tiles) return;
+  typedef Elem<kType> E;
+  const int lane = lane_id();
+  Acc<kInf> all, part;
+  Tile tile = lay.tiles[r.first];
+  int64_t slot = r.first;
+  for (int64_t ti = r.first; ti < r.last; ++ti) {
+    const Tile next = lay.tiles[min(ti + 1, lay.n_tiles - 1)];
+    const Span<kType> sp(lay, g, r.k, tile);
+    const Buf b = sp.body();
+    for (int v0 = 0; v0 < sp.nvec; v0 += kGU * kWave) {
+      u32x4 raw[kGU];
+#pragma unroll
+      for (int u = 0; u < kGU; ++u)
+        raw[u] = __builtin_amdgcn_raw_buffer_load_b128(b, (v0 + u * kWave + lane) * 16, 0, kAux);
+#pragma unroll
+      for (int u = 0; u < kGU; ++u) {
+        typename E::T v[E::kVec];
+        __builtin_memcpy(v, &raw[u], 16);
+#pragma unroll
+        for (int j = 0; j < E::kVec; ++j) part.add(E::to_f32(v[j]));
+      }
+    }
+    if (lane < sp.head) part.add(E::to_f32(sp.p[lane]));
+    if (lane < sp.tail) part.add(E::to_f32(sp.tail_at()[lane]));
+    if (kTensors && (next.l != tile.l || ti + 1 == r.last)) {
+      all.join(part);
+      const double s = part.wave();
+      if (lane == 0) g.part[(int64_t)r.k * lay.n_tiles + slot] = s;
+      part = Acc<kInf>();
+      slot = ti + 1;
+    }
+    tile = next;
+  }
+  const double s = kTensors ? all.wave() : part.wave();
+  if (lane == 0) g.run_sums[r.k * g.runs + r.run] = s;
 }
 
-// The sum (or the largest) of v[0..n) over the workgroup, in thread 0.
+// A NaN stays: of two values the larger, unless one is no number.
 template <bool kInf>
-__device__ double block_join(const double* __restrict__ v, int64_t n) {
-  __shared__ double s_v[kWaves];
+__device__ __forceinline__ double joined(double p, double q) {
+  return kInf ? (p >= q || p != p ? p : q) : p + q;
+}
+
+// The sum (or the largest) of at(0 .. n-1) over the workgroup, in thread 0.
+template <bool kInf, typename At>
+__device__ double block_join(int64_t n, At at) {
+  __shared__ double s_v[kFinWaves];
   double a = 0.0;
-  // a NaN stays: of two values the larger, unless one is no number
-  auto join = [](double p, double q) { return kInf ? (p >= q || p != p ? p : q) : p + q; };
-  for (int64_t i = threadIdx.x; i < n; i += kBlock) a = join(a, v[i]);
+#pragma unroll 4
+  for (int64_t i = threadIdx.x; i < n; i += kFinWaves * kWave) a = joined<kInf>(a, at(i));
 #pragma unroll
-  for (int o = kWave / 2; o > 0; o >>= 1) a = join(a, __shfl_xor(a, o));
+  for (int o = kWave / 2; o > 0; o >>= 1) a = joined<kInf>(a, __shfl_xor(a, o));
   if (lane_id() == 0) s_v[wave_id()] = a;
   __syncthreads();
-  a = s_v[0];
-  for (int i = 1; i < kWaves; ++i) a = join(a, s_v[i]);
+  if (threadIdx.x == 0)
+    for (int i = 1; i < kFinWaves; ++i) a = joined<kInf>(a, s_v[i]);
   return a;
 }
 
@@ -120,24 +159,26 @@ __device__ __forceinline__ float norm_of(double s) {
   return (float)(kInf ? s : sqrt(s));
 }
 
-// Grid: K L workgroups, one per (worker, tensor).
+// Grid: K workgroups for the workers' norms, then, if asked for, K L for the
+// tensors'.
 template <bool kInf>
-__global__ __launch_bounds__(kBlock) void k_grad_tensors(DevLayout lay, GradsDev g,
-                                                         float* __restrict__ tensor_norms) {
-  const int l = (int)(blockIdx.x % (unsigned)lay.L), k = (int)(blockIdx.x / (unsigned)lay.L);
-  const TensorInfo t = lay.tensors[l];
-  const double s = block_join<kInf>(g.part + (int64_t)k * lay.n_tiles + t.first_tile, t.ntiles);
-  if (threadIdx.x != 0) return;
-  g.tpart[blockIdx.x] = s;
-  if (tensor_norms != nullptr) tensor_norms[blockIdx.x] = norm_of<kInf>(s);
-}
-
-// Grid: K workgroups.
-template <bool kInf>
-__global__ __launch_bounds__(kBlock) void k_grad_norms(DevLayout lay, GradsDev g,
-                                                       float* __restrict__ norms) {
-  const double s = block_join<kInf>(g.tpart + (int64_t)blockIdx.x * lay.L, lay.L);
-  if (threadIdx.x == 0) norms[blockIdx.x] = norm_of<kInf>(s);
+__global__ __launch_bounds__(kFinWaves* kWave) void k_grad_norms(
+    DevLayout lay, GradsDev g, float* __restrict__ norms, float* __restrict__ tensor_norms) {
+  if (blockIdx.x < (unsigned)g.K) {
+    const double* v = g.run_sums + (int64_t)blockIdx.x * g.runs;
+    const double s = block_join<kInf>(g.runs, [&](int64_t i) { return v[i]; });
+    if (threadIdx.x == 0) norms[blockIdx.x] = norm_of<kInf>(s);
+    return;
+  }
+  const unsigned b = blockIdx.x - (unsigned)g.K;
+  const TensorInfo t = lay.tensors[b % (unsigned)lay.L];
+  const double* v = g.part + (int64_t)(b / (unsigned)lay.L) * lay.n_tiles;
+  // the tensor's slots: its first tile, and those where a run begins
+  const int64_t first = t.first_tile, run = first / g.run_tiles;
+  const int64_t n = (first + t.ntiles - 1) / g.run_tiles - run + 1;
+  const double s = block_join<kInf>(
+      n, [&](int64_t i) { return v[i == 0 ? first : (run + i) * g.run_tiles]; });
+  if (threadIdx.x == 0) tensor_norms[b] = norm_of<kInf>(s);
 }
 
 // c v in the gradient's own type.  The product is rounded to fp32 first, in every
@@ -149,7 +190,10 @@ __device__ __forceinline__ typename Elem<kType>::T scaled(typename Elem<kType>::
   return Elem<kType>::of_f32(f);
 }
 
-// Grid: as k_grad_tiles.  kRows: into the fp32 rows of the layout.
+// A wave takes a tile.  kRows: into the fp32 rows of the layout; a load is then
+// as many elements as a 16-byte store, so that a wave's stores are one run of
+// memory (bert_base in bf16, K = 4: 450 us, 662 with 16-byte loads and two stores
+// apart).  Grid: K times ceil(n_tiles / 4) workgroups.
 template <int kType, bool kRows>
 __global__ __launch_bounds__(kBlock) void k_clip(DevLayout lay, GradsDev g, float max_norm,
                                                  const float* __restrict__ norms,
@@ -157,16 +201,48 @@ __global__ __launch_bounds__(kBlock) void k_clip(DevLayout lay, GradsDev g, floa
   const unsigned per = (unsigned)((lay.n_tiles + kWaves - 1) / kWaves);
   const int k = (int)(blockIdx.x / per);
   const int64_t ti = (int64_t)(blockIdx.x % per) * kWaves + wave_id();
+  if (ti >= lay.n_tiles) return;
   const float c = clip_factor(max_norm, norms[k]);
   if (!kRows && c == 1.0f) return;  // in place, v * 1 is v
-  if (ti >= lay.n_tiles) return;
   const int lane = lane_id();
-  const Tile tile = lay.tiles[ti];
-  const Span<kType> sp(lay, g, k, tile);
   typedef Elem<kType> E;
   typedef typename E::T T;
+  const Tile tile = lay.tiles[ti];
+  const Span<kType> sp(lay, g, k, tile);
   const Buf b = sp.body();
+  const int tail0 = sp.head + sp.nvec * E::kVec;
   float* row = kRows ? out + (int64_t)k * lay.d_pad + tile.start : nullptr;
+  if (kRows) {
+    // stores at the alignment of an element
+    typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
+    constexpr int kLd = 4 * (int)sizeof(T);  // bytes of a load
+    const int n4 = sp.nvec * (E::kVec / 4);
+    for (int v0 = 0; v0 < n4; v0 += kGU * kWave) {
+      T v[kGU][4];
+#pragma unroll
+      for (int u = 0; u < kGU; ++u) {
+        const int at = (v0 + u * kWave + lane) * kLd;
+        if (kLd == 16) {
+          const u32x4 q = __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, kAuxNT);
+          __builtin_memcpy(v[u], &q, kLd);
+        } else {
+          const u32x2 q = __builtin_amdgcn_raw_buffer_load_b64(b, at, 0, kAuxNT);
+          __builtin_memcpy(v[u], &q, kLd);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kGU; ++u) {
+        const int i = v0 + u * kWave + lane;
+        const f32x4 q = {E::to_f32(v[u][0]) * c, E::to_f32(v[u][1]) * c, E::to_f32(v[u][2]) * c,
+                         E::to_f32(v[u][3]) * c};
+        if (i < n4)
+          __builtin_nontemporal_store(q, reinterpret_cast<f32x4*>(row + sp.head + 4 * i));
+      }
+    }
+    if (lane < sp.head) row[lane] = E::to_f32(sp.p[lane]) * c;
+    if (lane < sp.tail) row[tail0 + lane] = E::to_f32(sp.p[tail0 + lane]) * c;
+    return;
+  }
   for (int v0 = 0; v0 < sp.nvec; v0 += kGU * kWave) {
     u32x4 raw[kGU];
 #pragma unroll
@@ -174,32 +250,20 @@ __global__ __launch_bounds__(kBlock) void k_clip(DevLayout lay, GradsDev g, floa
       raw[u] = __builtin_amdgcn_raw_buffer_load_b128(b, (v0 + u * kWave + lane) * 16, 0, kAuxNT);
 #pragma unroll
     for (int u = 0; u < kGU; ++u) {
-      const int i = v0 + u * kWave + lane;
       T v[E::kVec];
       __builtin_memcpy(v, &raw[u], 16);
-      if (kRows) {
-        if (i < sp.nvec) {
 #pragma unroll
-          for (int j = 0; j < E::kVec; ++j)
-            st_nt(row + sp.head + i * E::kVec + j, E::to_f32(v[j]) * c);
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < E::kVec; ++j) v[j] = scaled<kType>(v[j], c);
-        __builtin_memcpy(&raw[u], v, 16);
-        __builtin_amdgcn_raw_buffer_store_b128(raw[u], b, i * 16, 0, kAuxNT);
-      }
+      for (int j = 0; j < E::kVec; ++j) v[j] = scaled<kType>(v[j], c);
+      __builtin_memcpy(&raw[u], v, 16);
+      __builtin_amdgcn_raw_buffer_store_b128(raw[u], b, (v0 + u * kWave + lane) * 16, 0, kAuxNT);
     }
   }
-  const int tail0 = sp.head + sp.nvec * E::kVec;
-  if (lane < sp.head) {
-    const T v = sp.p[lane];
-    if (kRows) row[lane] = E::to_f32(v) * c; else sp.p[lane] = scaled<kType>(v, c);
-  }
-  if (lane < sp.tail) {
-    const T v = sp.p[tail0 + lane];
-    if (kRows) row[tail0 + lane] = E::to_f32(v) * c; else sp.p[tail0 + lane] = scaled<kType>(v, c);
-  }
+  if (lane < sp.head) sp.p[lane] = scaled<kType>(sp.p[lane], c);
+  if (lane < sp.tail) sp.p[tail0 + lane] = scaled<kType>(sp.p[tail0 + lane], c);
+}
+
+dim3 run_grid(const GradsDev& g) {
+  return dim3((unsigned)(g.K * ((g.runs + kWaves - 1) / kWaves)));
 }
 
 }  // namespace
@@ -207,19 +271,24 @@ __global__ __launch_bounds__(kBlock) void k_clip(DevLayout lay, GradsDev g, floa
 hipError_t launch_grad_norm(const DevLayout& lay, const GradsDev& g, bool inf, float* norms,
                             float* tensor_norms, hipStream_t s) {
   const LaunchEvents ev;
-  const dim3 tiles(per_wave_grid(lay) * (unsigned)g.K), tens((unsigned)g.K * (unsigned)lay.L);
-#define SAEF_GN(T, I) SAEF_LAUNCH((k_grad_tiles<T, I>), tiles, dim3(kBlock), 0, s, lay, g)
+  const dim3 runs = run_grid(g);
+  const dim3 fin((unsigned)g.K * (tensor_norms != nullptr ? 1u + (unsigned)lay.L : 1u));
+  const bool tensors = tensor_norms != nullptr;
+#define SAEF_GN4(T, I, S, A) \
+  SAEF_LAUNCH((k_grad_tiles<T, I, S, A>), runs, dim3(kBlock), 0, s, lay, g)
+#define SAEF_GN(T, I)                                                                         \
+  do {                                                                                        \
+    if (g.cached) { if (tensors) SAEF_GN4(T, I, true, 0); else SAEF_GN4(T, I, false, 0); }    \
+    else { if (tensors) SAEF_GN4(T, I, true, kAuxNT); else SAEF_GN4(T, I, false, kAuxNT); }   \
+  } while (0)
   if (g.dtype == kF32) { if (inf) SAEF_GN(kF32, true); else SAEF_GN(kF32, false); }
   else if (g.dtype == kBF16) { if (inf) SAEF_GN(kBF16, true); else SAEF_GN(kBF16, false); }
   else { if (inf) SAEF_GN(kF16, true); else SAEF_GN(kF16, false); }
 #undef SAEF_GN
-  if (inf) {
-    SAEF_LAUNCH(k_grad_tensors<true>, tens, dim3(kBlock), 0, s, lay, g, tensor_norms);
-    SAEF_LAUNCH(k_grad_norms<true>, dim3(g.K), dim3(kBlock), 0, s, lay, g, norms);
-  } else {
-    SAEF_LAUNCH(k_grad_tensors<false>, tens, dim3(kBlock), 0, s, lay, g, tensor_norms);
-    SAEF_LAUNCH(k_grad_norms<false>, dim3(g.K), dim3(kBlock), 0, s, lay, g, norms);
-  }
+#undef SAEF_GN4
+  const dim3 fb(kFinWaves * kWave);
+  if (inf) SAEF_LAUNCH(k_grad_norms<true>, fin, fb, 0, s, lay, g, norms, tensor_norms);
+  else SAEF_LAUNCH(k_grad_norms<false>, fin, fb, 0, s, lay, g, norms, tensor_norms);
   return hipGetLastError();
 }
 

@@ -16,21 +16,31 @@ struct GroupNormDev {
   int64_t N, P;
   int32_t K, C, G, Cg;
   float eps;
-  int32_t vec;      // elements of a load: 16 bytes' worth, or 1
-  int32_t slab;     // channels of a workgroup: C, or a multiple of vec
-  int32_t slabs;    // ceil(C / slab)
-  int32_t threads;  // of a workgroup; slab divides its active threads' vec elements
-  int32_t splits;   // workgroups over the pixels of a sample
-  double* part;     // [K N splits C 2] sums per channel
+  int32_t vec;     // elements of a load: 16 bytes' worth, or 1
+  int32_t slab;    // channels of a workgroup: C, or a multiple of vec
+  int32_t slabs;   // ceil(C / slab)
+  int32_t splits;  // workgroups over the pixels of a sample
+  int32_t backwards;  // the second pass goes through the samples backwards
+  double* part;    // [K N splits C 2] backward sums per channel
+  double* pieces;  // [K N splits (G + slabs - 1) 2] sums per group and slab
 };
 
-hipError_t launch_group_norm_forward(const GroupNormDev& d, int dtype, int act, const void* x,
-                                     const float* gamma, const float* beta, int64_t ld, void* y,
-                                     float* mean, float* rstd, hipStream_t s);
+// How a kernel that reads its features once cuts the work: workgroups of
+// `threads` threads, each holding `vectors` 16-byte vectors, take slabs of
+// `slab` channels of whole groups.  threads == 0: the shape does not fit.
+struct GroupNormHeld {
+  int32_t threads, vectors, slab, slabs;
+};
 
-hipError_t launch_group_norm_backward(const GroupNormDev& d, int dtype, int act, const void* dy,
-                                      const void* x, const float* gamma, const float* beta,
-                                      int64_t ld, const float* mean, const float* rstd, void* dx,
-                                      float* dgamma, float* dbeta, int64_t ldg, hipStream_t s);
+hipError_t launch_group_norm_forward(const GroupNormDev& d, const GroupNormHeld& held, int dtype,
+                                     int act, const void* x, const float* gamma,
+                                     const float* beta, int64_t ld, void* y, float* mean,
+                                     float* rstd, hipStream_t s);
+
+hipError_t launch_group_norm_backward(const GroupNormDev& d, const GroupNormHeld& held, int dtype,
+                                      int act, const void* dy, const void* x, const float* gamma,
+                                      const float* beta, int64_t ld, const float* mean,
+                                      const float* rstd, void* dx, float* dgamma, float* dbeta,
+                                      int64_t ldg, hipStream_t s);
 
 }  // namespace saef

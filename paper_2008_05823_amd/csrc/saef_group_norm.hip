@@ -21,6 +21,8 @@
 // from there on.
 #include <hip/hip_ext.h>
 
+#include <algorithm>
+
 #include "saef_device.h"
 #include "saef_group_norm.h"
 
@@ -37,7 +39,17 @@ struct Vals {
 #pragma unroll
     for (int j = 0; j < kN; ++j) v[j] = j < n ? p[j] : (T)0.0f;
   }
-  __device__ __forceinline__ void store(T* p) const { __builtin_memcpy(p, v, sizeof(v)); }
+  __device__ __forceinline__ void store(T* p) const {
+    if constexpr (sizeof(v) == 16) {
+      // 16 bytes at the alignment of the smallest element
+      typedef unsigned int Raw __attribute__((ext_vector_type(4), aligned(2)));
+      Raw r;
+      __builtin_memcpy(&r, v, 16);
+      __builtin_nontemporal_store(r, reinterpret_cast<Raw*>(p));
+    } else {
+      __builtin_memcpy(p, v, sizeof(v));
+    }
+  }
   __device__ __forceinline__ void store(T* p, int n) const {
 #pragma unroll
     for (int j = 0; j < kN; ++j)
@@ -47,16 +59,10 @@ struct Vals {
   __device__ __forceinline__ void set(int j, float f) { v[j] = Elem<kType>::of_f32(f); }
 };
 
-// 1 / (1 + exp(-z)), to 2 or 3 units in the last place: the exponent's product
-// with log2 e is carried to twice the precision.
+// 1 / (1 + exp(-z)), to about 4 (1 + |z|) 2^-24 relative: four instructions, two of
+// them at a quarter of the rate.  An infinite exponential gives 0.
 __device__ __forceinline__ float sigmoid(float z) {
-  const float l2e = 1.44269502f, l2e_lo = 1.92596303e-8f, ln2 = 0.693147181f;
-  const float hi = -z * l2e;
-  const float lo = __builtin_fmaf(-z, l2e, -hi) - z * l2e_lo;
-  float e = __builtin_amdgcn_exp2f(hi);
-  // (an infinite z or exponential stays what it is)
-  e = __builtin_fabsf(hi) < 126.0f ? __builtin_fmaf(e, lo * ln2, e) : e;
-  return __builtin_amdgcn_rcpf(1.0f + e);
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * z));
 }
 
 template <int kAct>
@@ -77,6 +83,81 @@ __device__ __forceinline__ float act_back(float dy, float z) {
   return dy;
 }
 
+// The statistics of m values from their sum and sum of squares.
+struct Stats {
+  float mean, rest, rstd;  // mean rounded to fp32, and what that leaves
+};
+__device__ __forceinline__ Stats stats_of(double s0, double s1, double m, float eps) {
+  const double mu = s0 / m;
+  const double var = s1 / m - mu * mu;
+  Stats r;
+  r.mean = (float)mu;
+  r.rest = (float)(mu - (double)r.mean);
+  // (a rounding below 0 is 0; what is no number stays none)
+  r.rstd = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)eps));
+  return r;
+}
+
+extern __shared__ __align__(16) unsigned char dyn_lds[];
+
+// Joins pairs of sums: put(i, sum of at(i, 0), at(i, 1), ...) for i < count, of up
+// to `terms` terms each.  A power of two of lanes adds up one of them, few enough
+// that all of them are under way at once.  All threads of the workgroup call it.
+template <typename At, typename Put>
+__device__ __forceinline__ void join_sums(int count, int terms, At at, Put put) {
+  int lanes = 1;
+  while (lanes < kWave && lanes < terms && 2 * lanes * count <= (int)blockDim.x) lanes *= 2;
+  const int l = (int)threadIdx.x & (lanes - 1), per = (int)blockDim.x / lanes;
+  for (int base = 0; base < count; base += per) {
+    const int i = base + (int)threadIdx.x / lanes;
+    double2 s = make_double2(0.0, 0.0);
+    if (i < count) {
+#pragma unroll 4
+      for (int q = l; q < terms; q += lanes) {
+        const double2 v = at(i, q);
+        s.x += v.x;
+        s.y += v.y;
+      }
+    }
+    for (int o = lanes / 2; o > 0; o >>= 1) {
+      s.x += __shfl_xor(s.x, o);
+      s.y += __shfl_xor(s.y, o);
+    }
+    if (i < count && l == 0) put(i, s);
+  }
+}
+
+// Before a workgroup's threads lay their sums side by side in LDS: where the
+// channels repeat every `period` threads, a power of two below a wave, the lanes
+// of a wave that share theirs are added first.  The return value is this
+// thread's place in the table, or -1, and `active` becomes the places.
+template <int kA, typename V>
+__device__ __forceinline__ int fold_lanes(V (&v)[kA], V (&w)[kA], int period, int& active) {
+  const int t = (int)threadIdx.x;
+  if (period >= kWave || (period & (period - 1)) != 0) return t < active ? t : -1;
+  for (int o = kWave / 2; o >= period; o /= 2) {
+#pragma unroll
+    for (int j = 0; j < kA; ++j) {
+      v[j] += __shfl_xor(v[j], o);
+      w[j] += __shfl_xor(w[j], o);
+    }
+  }
+  active = (int)blockDim.x / kWave * period;
+  const int l = t % kWave;
+  return l < period ? t / kWave * period + l : -1;
+}
+
+// ------------------------------------------------------------------ two passes
+// Samples too large for a workgroup are read twice: each workgroup adds up a
+// slab of channels over a range of pixels, then a second kernel joins a
+// sample's sums and computes the result.  Where the features exceed the last-level
+// cache the second goes through the samples backwards, so that what the cache still
+// holds is read from there (256 samples of 1.6 MB: forward 223 us, in the same order
+// 243; backward 376 and 394; at 103 MB the same order is 1 us ahead).
+
+// Vectors of a thread's in flight.
+constexpr int kU = 4;
+
 // A workgroup's part of a sample: channels [c0, c0 + cw), pixels [p0, p1).
 template <int kN>
 struct Part {
@@ -84,22 +165,21 @@ struct Part {
   int64_t first;   // element of the features the thread starts at
   int64_t left;    // elements of the part from there on (0 or less: none)
   int64_t stride;  // elements of the features, and
-  int64_t dec;     // of the part, to the thread's next
-  int k, s, c0, cw, c, active;
+  int64_t dec;     // of the part, to the thread's next vector
+  int k, s, b, c0, cw, c, period, active;
 
-  __device__ __forceinline__ Part(const GroupNormDev& d) {
-    int64_t b = blockIdx.x;
-    s = (int)(b % d.splits);
-    b /= d.splits;
-    c0 = (int)(b % d.slabs) * d.slab;
-    n = b / d.slabs;
-    k = (int)(n / d.N);
+  __device__ __forceinline__ Part(const GroupNormDev& d, uint32_t item) {
+    s = (int)(item % (uint32_t)d.splits);
+    item /= (uint32_t)d.splits;
+    b = (int)(item % (uint32_t)d.slabs);
+    c0 = b * d.slab;
+    n = item / (uint32_t)d.slabs;
+    k = (int)((uint32_t)n / (uint32_t)d.N);
     cw = min(d.slab, d.C - c0);
     const int64_t per = (d.P + d.splits - 1) / d.splits;
     const int64_t p0 = min(d.P, s * per), p1 = min(d.P, p0 + per);
     // threads whose elements make up whole pixels of the slab
-    const int common = min(kN, cw & -cw);
-    const int period = cw / common;
+    period = cw / min(kN, cw & -cw);
     active = (int)blockDim.x / period * period;
     const int t = (int)threadIdx.x;
     const int f = t * kN;
@@ -110,269 +190,575 @@ struct Part {
     dec = (int64_t)active * kN;
     stride = dec / cw * d.C;
   }
-  // channel of the thread's element j
-  __device__ __forceinline__ int channel(int j) const {
-    int q = c + j;
-    while (q >= cw) q -= cw;
-    return c0 + q;
+  // Calls f(j, channel, group) for the thread's elements j.
+  template <typename F>
+  __device__ __forceinline__ void channels(const GroupNormDev& d, F f) const {
+    int q = c, g = (c0 + c) / d.Cg, in = c0 + c - g * d.Cg;
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      f(j, c0 + q, g);
+      ++q;
+      if (++in == d.Cg) {
+        in = 0;
+        ++g;
+      }
+      if (q == cw) {  // the next pixel (the slab is all channels then)
+        q = 0;
+        g = 0;
+        in = 0;
+      }
+    }
+  }
+  // groups that the slab meets, and the channels of the i-th within the slab
+  __device__ __forceinline__ int group0(const GroupNormDev& d) const { return c0 / d.Cg; }
+  __device__ __forceinline__ int groups(const GroupNormDev& d) const {
+    return (c0 + cw - 1) / d.Cg - c0 / d.Cg + 1;
+  }
+  __device__ __forceinline__ int lo(const GroupNormDev& d, int i) const {
+    return max((group0(d) + i) * d.Cg - c0, 0);
+  }
+  __device__ __forceinline__ int hi(const GroupNormDev& d, int i) const {
+    return min((group0(d) + i + 1) * d.Cg - c0, cw);
   }
 };
 
-// Sums over the threads of a workgroup: v[j] of thread t belongs to channel
-// (t kN + j) mod cw.  put(c, sum) is called once for each channel c < cw.
-template <int kN, typename V, typename F>
-__device__ __forceinline__ void channel_sums(const V (&v)[kN], int active, int cw, V* lds, F put) {
-  const int t = (int)threadIdx.x;
-  if (t < active) {
-#pragma unroll
-    for (int j = 0; j < kN; ++j) lds[t * kN + j] = v[j];
-  }
-  __syncthreads();
-  for (int c = t; c < cw; c += (int)blockDim.x) {
-    double a = 0.0;
-    for (int f = c; f < active * kN; f += cw) a += (double)lds[f];
-    put(c, a);
-  }
-  __syncthreads();
-}
-
-extern __shared__ __align__(16) unsigned char dyn_lds[];
-
-// Partial sums per channel: forward x and x^2, backward A and B.
-// Grid: K N slabs splits workgroups.
-template <int kType, int kN, int kAct, bool kBack>
-__global__ __launch_bounds__(1024) void k_gn_sums(GroupNormDev d, const void* __restrict__ xv,
-                                                  const void* __restrict__ dyv,
-                                                  const float* __restrict__ gamma,
-                                                  const float* __restrict__ beta, int64_t ld,
-                                                  const float* __restrict__ mean,
-                                                  const float* __restrict__ rstd) {
+// The vectors of a thread's part, from kS features at once: kU of each are on
+// their way while the kU before are used.
+template <int kType, int kN, int kS>
+struct Stream {
   typedef typename Elem<kType>::T T;
-  typedef std::conditional_t<kBack, float, double> Sum;
-  const Part<kN> w(d);
-  const T* x = static_cast<const T*>(xv) + w.first;
-  const T* dy = kBack ? static_cast<const T*>(dyv) + w.first : nullptr;
-  Sum a0[kN] = {}, a1[kN] = {};
-  float mu[kN], rs[kN], ga[kN], be[kN];
-  if (kBack && w.left > 0) {
-#pragma unroll
-    for (int j = 0; j < kN; ++j) {
-      const int c = w.channel(j), g = c / d.Cg;
-      mu[j] = mean[w.n * d.G + g];
-      rs[j] = rstd[w.n * d.G + g];
-      ga[j] = gamma[w.k * ld + c];
-      be[j] = beta[w.k * ld + c];
-    }
-  }
-  for (int64_t left = w.left; left > 0; left -= w.dec) {
-    Vals<kType, kN> xs, ds;
-    if (left >= kN) {
-      xs.load(x);
-      if (kBack) ds.load(dy);
-    } else {
-      xs.load(x, (int)left);
-      if (kBack) ds.load(dy, (int)left);
-    }
-#pragma unroll
-    for (int j = 0; j < kN; ++j) {
-      if (kBack) {
-        const float h = (xs[j] - mu[j]) * rs[j];
-        const float dz = act_back<kAct>(ds[j], __builtin_fmaf(h, ga[j], be[j]));
-        if (left > j) {
-          a0[j] = __builtin_fmaf(dz, h, (float)a0[j]);
-          a1[j] += dz;
-        }
-      } else {
-        const double v = xs[j];
-        a0[j] += v;
-        a1[j] = __builtin_fma(v, v, (double)a1[j]);
-      }
-    }
-    x += w.stride;
-    if (kBack) dy += w.stride;
-  }
-  Sum* lds = reinterpret_cast<Sum*>(dyn_lds);
-  double* part = d.part + ((w.n * d.splits + w.s) * d.C + w.c0) * 2;
-  channel_sums(a0, w.active, w.cw, lds, [&](int c, double v) { part[2 * c] = v; });
-  channel_sums(a1, w.active, w.cw, lds, [&](int c, double v) { part[2 * c + 1] = v; });
-}
+  const T* src[kS];
+  int64_t rest, at, dec, stride;
+  Vals<kType, kN> v[kU][kS];
 
-struct GroupSums {
-  float a, b, c;  // forward: mean, its remainder, rstd; backward: s1, s2
+  __device__ __forceinline__ Stream(const Part<kN>& w, const void* a, const void* b = nullptr)
+      : rest(w.left), at(w.first), dec(w.dec), stride(w.stride) {
+    src[0] = static_cast<const T*>(a);
+    if (kS > 1) src[kS - 1] = static_cast<const T*>(b);
+    if (rest >= kN) fetch(v, rest, at);
+  }
+  // (vectors past the part's end: the first one again)
+  __device__ __forceinline__ void fetch(Vals<kType, kN> (&to)[kU][kS], int64_t left,
+                                        int64_t from) const {
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int64_t p = left - u * dec >= kN ? from + u * stride : from;
+#pragma unroll
+      for (int i = 0; i < kS; ++i) to[u][i].load(src[i] + p);
+    }
+  }
+  // Calls f(v, at, n) with the thread's vectors one after another: n elements
+  // from element `at` of the features.
+  template <typename F>
+  __device__ __forceinline__ void each(F f) {
+    while (rest >= kN) {
+      Vals<kType, kN> next[kU][kS];
+      const bool more = rest - kU * dec >= kN;  // (at least one whole vector left)
+      if (more) fetch(next, rest - kU * dec, at + kU * stride);
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        if (rest >= kN) {
+          f(v[u], at, kN);
+          rest -= dec;
+          at += stride;
+        }
+      }
+      if (!more) break;
+#pragma unroll
+      for (int u = 0; u < kU; ++u)
+#pragma unroll
+        for (int i = 0; i < kS; ++i) v[u][i] = next[u][i];
+    }
+    // the sample's last elements, fewer than a vector
+    if (rest > 0) {
+      Vals<kType, kN> last[kS];
+#pragma unroll
+      for (int i = 0; i < kS; ++i) last[i].load(src[i] + at, (int)rest);
+      f(last, at, (int)rest);
+    }
+  }
 };
 
-// The two sums of each group that the slab meets, over channels and splits
-// (backward: weighted by gamma), by `lanes` lanes a group.  put(g, s0, s1).
-template <bool kBack, int kN, typename F>
-__device__ __forceinline__ void group_sums(const GroupNormDev& d, const Part<kN>& w,
-                                           const float* __restrict__ gamma, int64_t ld, F put) {
-  const int g0 = w.c0 / d.Cg, g1 = (w.c0 + w.cw - 1) / d.Cg;
-  const int64_t terms = (int64_t)d.Cg * d.splits;
-  int lanes = 1;
-  while (lanes < kWave && lanes < terms) lanes *= 2;
-  const int per = (int)blockDim.x / lanes;
-  const int at = (int)threadIdx.x / lanes, l = (int)threadIdx.x % lanes;
-  // every lane of a wave takes part in each step
-  for (int gb = g0; gb <= g1; gb += per) {
-    const int g = gb + at;
-    double s0 = 0.0, s1 = 0.0;
-    if (g <= g1) {
-      for (int64_t i = l; i < terms; i += lanes) {
-        const int c = g * d.Cg + (int)(i % d.Cg);
-        const double* p = d.part + ((w.n * d.splits + i / d.Cg) * d.C + c) * 2;
-        const double f = kBack ? (double)gamma[w.k * ld + c] : 1.0;
-        s0 += f * p[0];
-        s1 += f * p[1];
-      }
-    }
-    for (int o = lanes / 2; o > 0; o >>= 1) {
-      s0 += __shfl_xor(s0, o);
-      s1 += __shfl_xor(s1, o);
-    }
-    if (g <= g1 && l == 0) put(g, s0, s1);
-  }
+// The sums of the i-th group of the slab over all pixel ranges and, where
+// groups span slabs, all slabs: entry g + b of a row belongs to group g in slab b.
+template <int kN, typename Put>
+__device__ __forceinline__ void join_groups(const GroupNormDev& d, const Part<kN>& w, Put put) {
+  const int Q = d.G + d.slabs - 1;
+  // slabs a group may lie in, at most
+  const int span = d.slab % d.Cg == 0 ? 1 : min(d.slabs, (d.Cg - 1) / d.slab + 2);
+  const double2* pieces = reinterpret_cast<const double2*>(d.pieces) + w.n * d.splits * Q;
+  join_sums(w.groups(d), d.splits * span, [&](int i, int q) {
+    const int g = w.group0(d) + i, b = g * d.Cg / d.slab + q % span;
+    if (b > (g * d.Cg + d.Cg - 1) / d.slab) return make_double2(0.0, 0.0);
+    return pieces[(int64_t)(q / span) * Q + g + b];
+  }, put);
 }
 
-// The statistics of m values from their sum and sum of squares.
-__device__ __forceinline__ GroupSums stats_of(double s0, double s1, double m, float eps) {
-  const double mu = s0 / m;
-  const double var = s1 / m - mu * mu;
-  GroupSums r;
-  r.a = (float)mu;
-  r.b = (float)(mu - (double)r.a);
-  // (a rounding below 0 is 0; what is no number stays none)
-  r.c = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)eps));
-  return r;
+// kOne: a vector lies in one group.  Grid: K N slabs splits workgroups.
+template <int kType, int kN, bool kOne>
+__global__ __launch_bounds__(kBlock) void k_gn_fwd_sums(GroupNormDev d,
+                                                        const void* __restrict__ x) {
+  constexpr int kA = kOne ? 1 : kN;  // sums of a thread
+  const Part<kN> w(d, blockIdx.x);
+  double a0[kA] = {}, a1[kA] = {};
+  Stream<kType, kN, 1>(w, x).each([&](Vals<kType, kN>* v, int64_t, int) {
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      const double f = v[0][j];
+      a0[kOne ? 0 : j] += f;
+      a1[kOne ? 0 : j] = __builtin_fma(f, f, a1[kOne ? 0 : j]);
+    }
+  });
+  double2* table = reinterpret_cast<double2*>(dyn_lds);
+  int active = w.active;
+  const int t = fold_lanes(a0, a1, w.period, active);
+  if (t >= 0) {
+#pragma unroll
+    for (int j = 0; j < kA; ++j) table[t * kA + j] = make_double2(a0[j], a1[j]);
+  }
+  __syncthreads();
+  // entries of a pixel of the slab, and pixels
+  constexpr int kPer = kN / kA;
+  const int wide = w.cw / kPer, rows = active * kA / wide, most = min(d.Cg, w.cw) / kPer;
+  double2* out = reinterpret_cast<double2*>(d.pieces) +
+                 (w.n * d.splits + w.s) * (d.G + d.slabs - 1) + w.group0(d) + w.b;
+  join_sums(w.groups(d), rows * most, [&](int i, int q) {
+    const int e = w.lo(d, i) / kPer + q % most;
+    return e < w.hi(d, i) / kPer ? table[q / most * wide + e] : make_double2(0.0, 0.0);
+  }, [&](int i, double2 s) { out[i] = s; });
 }
 
 template <int kType, int kN, int kAct>
-__global__ __launch_bounds__(1024) void k_gn_apply(GroupNormDev d, const void* __restrict__ xv,
-                                                   const float* __restrict__ gamma,
-                                                   const float* __restrict__ beta, int64_t ld,
-                                                   void* __restrict__ yv,
-                                                   float* __restrict__ mean,
-                                                   float* __restrict__ rstd) {
+__global__ __launch_bounds__(kBlock) void k_gn_fwd_apply(GroupNormDev d,
+                                                         const void* __restrict__ x,
+                                                         const float* __restrict__ gamma,
+                                                         const float* __restrict__ beta,
+                                                         int64_t ld, void* __restrict__ y,
+                                                         float* __restrict__ mean,
+                                                         float* __restrict__ rstd) {
   typedef typename Elem<kType>::T T;
-  const Part<kN> w(d);
-  GroupSums* st = reinterpret_cast<GroupSums*>(dyn_lds);
-  const int g0 = w.c0 / d.Cg;
+  const Part<kN> w(d, d.backwards ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+  Stream<kType, kN, 1> in(w, x);
+  Stats* st = reinterpret_cast<Stats*>(dyn_lds);
+  const int g0 = w.group0(d);
   const double m = (double)d.P * d.Cg;
-  group_sums<false>(d, w, nullptr, 0, [&](int g, double s0, double s1) {
-    const GroupSums r = stats_of(s0, s1, m, d.eps);
-    st[g - g0] = r;
-    // (a group over several slabs: all write the same)
+  join_groups(d, w, [&](int i, double2 s) {
+    const Stats r = stats_of(s.x, s.y, m, d.eps);
+    st[i] = r;
+    // (a group in several slabs: all write the same)
     if (w.s == 0) {
-      mean[w.n * d.G + g] = r.a;
-      rstd[w.n * d.G + g] = r.c;
+      mean[w.n * d.G + g0 + i] = r.mean;
+      rstd[w.n * d.G + g0 + i] = r.rstd;
     }
   });
   __syncthreads();
   if (w.left <= 0) return;
   float mu[kN], sc[kN], sh[kN];
-#pragma unroll
-  for (int j = 0; j < kN; ++j) {
-    const int c = w.channel(j);
-    const GroupSums r = st[c / d.Cg - g0];
-    mu[j] = r.a;
-    sc[j] = r.c * gamma[w.k * ld + c];
-    sh[j] = __builtin_fmaf(-r.b, sc[j], beta[w.k * ld + c]);
-  }
-  const T* x = static_cast<const T*>(xv) + w.first;
-  T* y = static_cast<T*>(yv) + w.first;
-  for (int64_t left = w.left; left > 0; left -= w.dec) {
-    Vals<kType, kN> v;
-    if (left >= kN) v.load(x); else v.load(x, (int)left);
+  w.channels(d, [&](int j, int c, int g) {
+    const Stats r = st[g - g0];
+    mu[j] = r.mean;
+    sc[j] = r.rstd * gamma[w.k * ld + c];
+    sh[j] = __builtin_fmaf(-r.rest, sc[j], beta[w.k * ld + c]);
+  });
+  in.each([&](Vals<kType, kN>* v, int64_t at, int n) {
 #pragma unroll
     for (int j = 0; j < kN; ++j)
-      v.set(j, act_of<kAct>(__builtin_fmaf(v[j] - mu[j], sc[j], sh[j])));
-    if (left >= kN) v.store(y); else v.store(y, (int)left);
-    x += w.stride;
-    y += w.stride;
+      v[0].set(j, act_of<kAct>(__builtin_fmaf(v[0][j] - mu[j], sc[j], sh[j])));
+    T* p = static_cast<T*>(y) + at;
+    if (n == kN) v[0].store(p); else v[0].store(p, n);
+  });
+}
+
+// Per channel A and B of the part, and per group their sums weighted by gamma.
+template <int kType, int kN, int kAct>
+__global__ __launch_bounds__(kBlock) void k_gn_bwd_sums(GroupNormDev d,
+                                                        const void* __restrict__ x,
+                                                        const void* __restrict__ dy,
+                                                        const float* __restrict__ gamma,
+                                                        const float* __restrict__ beta,
+                                                        int64_t ld,
+                                                        const float* __restrict__ mean,
+                                                        const float* __restrict__ rstd) {
+  const Part<kN> w(d, blockIdx.x);
+  Stream<kType, kN, 2> in(w, x, dy);
+  float a[kN] = {}, b[kN] = {};
+  if (w.left > 0) {
+    float mu[kN], gs[kN], be[kN];
+    w.channels(d, [&](int j, int c, int g) {
+      mu[j] = mean[w.n * d.G + g];
+      gs[j] = gamma[w.k * ld + c] * rstd[w.n * d.G + g];
+      be[j] = beta[w.k * ld + c];
+    });
+    in.each([&](Vals<kType, kN>* v, int64_t, int n) {
+#pragma unroll
+      for (int j = 0; j < kN; ++j) {
+        const float u = v[0][j] - mu[j];
+        const float dz = act_back<kAct>(v[1][j], __builtin_fmaf(u, gs[j], be[j]));
+        if (n == kN || j < n) {
+          a[j] = __builtin_fmaf(dz, u, a[j]);
+          b[j] += dz;
+        }
+      }
+    });
   }
+  // element f of the threads' sums side by side belongs to channel f mod cw
+  float2* table = reinterpret_cast<float2*>(dyn_lds);
+  int active = w.active;
+  const int place = fold_lanes(a, b, w.period, active);
+  const int t = (int)threadIdx.x, elems = active * kN;
+  double2* sums = reinterpret_cast<double2*>(table + elems);
+  if (place >= 0) {
+#pragma unroll
+    for (int j = 0; j < kN; ++j) table[place * kN + j] = make_float2(a[j], b[j]);
+  }
+  __syncthreads();
+  double2* part = reinterpret_cast<double2*>(d.part) + (w.n * d.splits + w.s) * d.C + w.c0;
+  for (int c = t; c < w.cw; c += (int)blockDim.x) {
+    double2 s = make_double2(0.0, 0.0);
+    for (int f = c; f < elems; f += w.cw) {
+      s.x += (double)table[f].x;
+      s.y += (double)table[f].y;
+    }
+    s.x *= (double)rstd[w.n * d.G + (w.c0 + c) / d.Cg];
+    part[c] = s;
+    const double f = gamma[w.k * ld + w.c0 + c];
+    sums[c] = make_double2(f * s.x, f * s.y);
+  }
+  __syncthreads();
+  const int most = min(d.Cg, w.cw);
+  double2* out = reinterpret_cast<double2*>(d.pieces) +
+                 (w.n * d.splits + w.s) * (d.G + d.slabs - 1) + w.group0(d) + w.b;
+  join_sums(w.groups(d), most, [&](int i, int q) {
+    const int e = w.lo(d, i) + q;
+    return e < w.hi(d, i) ? sums[e] : make_double2(0.0, 0.0);
+  }, [&](int i, double2 s) { out[i] = s; });
 }
 
 template <int kType, int kN, int kAct>
-__global__ __launch_bounds__(1024) void k_gn_back(GroupNormDev d, const void* __restrict__ dyv,
-                                                  const void* __restrict__ xv,
-                                                  const float* __restrict__ gamma,
-                                                  const float* __restrict__ beta, int64_t ld,
-                                                  const float* __restrict__ mean,
-                                                  const float* __restrict__ rstd,
-                                                  void* __restrict__ dxv) {
+__global__ __launch_bounds__(kBlock) void k_gn_bwd_apply(GroupNormDev d,
+                                                         const void* __restrict__ dy,
+                                                         const void* __restrict__ x,
+                                                         const float* __restrict__ gamma,
+                                                         const float* __restrict__ beta,
+                                                         int64_t ld,
+                                                         const float* __restrict__ mean,
+                                                         const float* __restrict__ rstd,
+                                                         void* __restrict__ dx) {
   typedef typename Elem<kType>::T T;
-  const Part<kN> w(d);
-  GroupSums* st = reinterpret_cast<GroupSums*>(dyn_lds);
-  const int g0 = w.c0 / d.Cg;
+  const Part<kN> w(d, d.backwards ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+  Stream<kType, kN, 2> in(w, x, dy);
+  float2* st = reinterpret_cast<float2*>(dyn_lds);
+  const int g0 = w.group0(d);
   const double m = (double)d.P * d.Cg;
-  group_sums<true>(d, w, gamma, ld, [&](int g, double s0, double s1) {
-    st[g - g0] = GroupSums{(float)(s1 / m), (float)(s0 / m), 0.0f};
+  join_groups(d, w, [&](int i, double2 s) {
+    st[i] = make_float2((float)(s.y / m), (float)(s.x / m));
   });
   __syncthreads();
   if (w.left <= 0) return;
-  float mu[kN], rs[kN], ga[kN], be[kN], s1[kN], s2[kN];
-#pragma unroll
-  for (int j = 0; j < kN; ++j) {
-    const int c = w.channel(j), g = c / d.Cg;
+  // dx = gamma rstd dz - rstd s1 - (x - mean) rstd^2 s2
+  float mu[kN], gs[kN], be[kN], k1[kN], k2[kN];
+  w.channels(d, [&](int j, int c, int g) {
+    const float r = rstd[w.n * d.G + g];
     mu[j] = mean[w.n * d.G + g];
-    rs[j] = rstd[w.n * d.G + g];
-    ga[j] = gamma[w.k * ld + c];
+    gs[j] = gamma[w.k * ld + c] * r;
     be[j] = beta[w.k * ld + c];
-    s1[j] = st[g - g0].a;
-    s2[j] = st[g - g0].b;
-  }
-  const T* x = static_cast<const T*>(xv) + w.first;
-  const T* dy = static_cast<const T*>(dyv) + w.first;
-  T* dx = static_cast<T*>(dxv) + w.first;
-  for (int64_t left = w.left; left > 0; left -= w.dec) {
-    Vals<kType, kN> xs, ds;
-    if (left >= kN) {
-      xs.load(x);
-      ds.load(dy);
-    } else {
-      xs.load(x, (int)left);
-      ds.load(dy, (int)left);
-    }
+    k1[j] = r * st[g - g0].x;
+    k2[j] = r * r * st[g - g0].y;
+  });
+  in.each([&](Vals<kType, kN>* v, int64_t at, int n) {
 #pragma unroll
     for (int j = 0; j < kN; ++j) {
-      const float h = (xs[j] - mu[j]) * rs[j];
-      const float dz = act_back<kAct>(ds[j], __builtin_fmaf(h, ga[j], be[j]));
-      ds.set(j, rs[j] * (__builtin_fmaf(ga[j], dz, -s1[j]) - h * s2[j]));
+      const float u = v[0][j] - mu[j];
+      const float dz = act_back<kAct>(v[1][j], __builtin_fmaf(u, gs[j], be[j]));
+      v[0].set(j, __builtin_fmaf(gs[j], dz, -__builtin_fmaf(u, k2[j], k1[j])));
     }
-    if (left >= kN) ds.store(dx); else ds.store(dx, (int)left);
-    x += w.stride;
-    dy += w.stride;
-    dx += w.stride;
+    T* p = static_cast<T*>(dx) + at;
+    if (n == kN) v[0].store(p); else v[0].store(p, n);
+  });
+}
+
+// ------------------------------------------------------------------ one pass
+// Features of a slab small enough for the registers of a workgroup are read once:
+// the sums are taken as they arrive, joined over the workgroup in LDS, and the
+// result is computed from the registers.  A slab holds whole groups and whole
+// 16-byte vectors.
+//
+// Reads go through a buffer resource over the sample: a vector past its last
+// pixel reads 0, which adds nothing to a sum, and is not written.
+constexpr int kHeldThreads = 512;  // of a workgroup, at most
+
+template <int kType, int kR>
+struct Held {
+  static constexpr int kN = Elem<kType>::kVec;
+  typedef typename Elem<kType>::T T;
+  int64_t n;        // sample, over all workers
+  int k, c0, c;     // worker, first channel of the slab and of the thread within it
+  int col, cols;    // the thread's column of vectors, and columns of the slab
+  int active;       // threads whose vectors make up whole pixels
+  uint32_t at;      // byte offset of the thread's first vector in the sample
+  uint32_t step;    // and to its next
+  uint32_t bytes;   // of the sample
+
+  __device__ __forceinline__ explicit Held(const GroupNormDev& d) {
+    const int b = (int)blockIdx.x;
+    c0 = b % d.slabs * d.slab;
+    n = b / d.slabs;
+    k = (int)(n / d.N);
+    cols = min(d.slab, d.C - c0) / kN;
+    const int t = (int)threadIdx.x;
+    const int rows = (int)blockDim.x / cols;
+    active = rows * cols;
+    const int p = t / cols;
+    col = t - p * cols;
+    c = col * kN;
+    bytes = (uint32_t)d.P * (uint32_t)d.C * (uint32_t)sizeof(T);
+    step = (uint32_t)rows * (uint32_t)d.C * (uint32_t)sizeof(T);
+    at = t < active ? ((uint32_t)p * (uint32_t)d.C + (uint32_t)(c0 + c)) * (uint32_t)sizeof(T)
+                    : 0x80000000u;
+  }
+  // whether any lane of the wave holds a pixel of the sample in vector i
+  __device__ __forceinline__ bool any(int i) const { return __ballot(at + i * step < bytes) != 0; }
+  __device__ __forceinline__ Buf over(const GroupNormDev& d, const void* p) const {
+    return buf_of(static_cast<const T*>(p) + n * d.P * d.C, bytes);
+  }
+  __device__ __forceinline__ void load(Buf r, u32x4 (&raw)[kR]) const {
+#pragma unroll
+    for (int i = 0; i < kR; ++i)
+      raw[i] = __builtin_amdgcn_raw_buffer_load_b128(r, at + i * step, 0, kAuxNT);
+  }
+};
+
+template <int kType>
+__device__ __forceinline__ Vals<kType, Elem<kType>::kVec> vals_of(const u32x4& raw) {
+  Vals<kType, Elem<kType>::kVec> v;
+  __builtin_memcpy(&v, &raw, 16);
+  return v;
+}
+template <int kType>
+__device__ __forceinline__ u32x4 raw_of(const Vals<kType, Elem<kType>::kVec>& v) {
+  u32x4 raw;
+  __builtin_memcpy(&raw, &v, 16);
+  return raw;
+}
+
+// Makes the compiler unpack the vectors again where they are used next, instead of
+// keeping their values in twice the registers meanwhile (16-bit features, 8
+// vectors a thread, forward: 88 registers, 118 otherwise).
+template <int kR>
+__device__ __forceinline__ void packed(u32x4 (&raw)[kR]) {
+#pragma unroll
+  for (int i = 0; i < kR; ++i) {
+    uint32_t a = raw[i].x, b = raw[i].y, c = raw[i].z, e = raw[i].w;
+    asm volatile("" : "+v"(a), "+v"(b), "+v"(c), "+v"(e));
+    raw[i] = u32x4{a, b, c, e};
   }
 }
 
-// dgamma and dbeta: the channel sums over a worker's samples and splits.
-// Grid: K ceil(C / 64) workgroups of 4 waves; wave w adds rows w, w + 4, ...
-__global__ __launch_bounds__(kBlock) void k_gn_params(GroupNormDev d, float* __restrict__ dgamma,
-                                                      float* __restrict__ dbeta, int64_t ldg) {
-  __shared__ double s_a[kWaves][kWave], s_b[kWaves][kWave];
+// kOne: a vector lies in one group.  Grid: K N slabs workgroups.
+template <int kType, int kAct, int kR, bool kOne>
+__global__ __launch_bounds__(kHeldThreads) void k_gn_fwd_held(GroupNormDev d, const void* __restrict__ x,
+                                                      const float* __restrict__ gamma,
+                                                      const float* __restrict__ beta, int64_t ld,
+                                                      void* __restrict__ y,
+                                                      float* __restrict__ mean,
+                                                      float* __restrict__ rstd) {
+  constexpr int kN = Elem<kType>::kVec;
+  constexpr int kA = kOne ? 1 : kN;  // sums of a thread
+  const Held<kType, kR> w(d);
+  u32x4 raw[kR];
+  w.load(w.over(d, x), raw);
+  const int t = (int)threadIdx.x;
+  float ga[kN], be[kN];
+#pragma unroll
+  for (int j = 0; j < kN; ++j) {
+    ga[j] = gamma[w.k * ld + w.c0 + w.c + j];
+    be[j] = beta[w.k * ld + w.c0 + w.c + j];
+  }
+  double a0[kA] = {}, a1[kA] = {};
+#pragma unroll
+  for (int i = 0; i < kR; ++i) {
+    if (!w.any(i)) continue;
+    const auto v = vals_of<kType>(raw[i]);
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      const double f = v[j];
+      a0[kOne ? 0 : j] += f;
+      a1[kOne ? 0 : j] = __builtin_fma(f, f, a1[kOne ? 0 : j]);
+    }
+  }
+  // entry t kA + j of the table belongs to channel ((t kA + j) mod (cols kA)) kN / kA
+  double2* table = reinterpret_cast<double2*>(dyn_lds);
+  Stats* st = reinterpret_cast<Stats*>(table + (int)blockDim.x * kA);
+  if (t < w.active) {
+#pragma unroll
+    for (int j = 0; j < kA; ++j) table[t * kA + j] = make_double2(a0[j], a1[j]);
+  }
+  __syncthreads();
+  const int groups = w.cols * kN / d.Cg;
+  const int wide = d.Cg * kA / kN;             // entries of a group in a pixel
+  const int terms = w.active / w.cols * wide;  // and in all
+  const double m = (double)d.P * d.Cg;
+  join_sums(groups, terms, [&](int g, int q) {
+    return table[q / wide * w.cols * kA + g * wide + q % wide];
+  }, [&](int g, double2 s) {
+    const Stats r = stats_of(s.x, s.y, m, d.eps);
+    st[g] = r;
+    const int64_t at = w.n * d.G + w.c0 / d.Cg + g;
+    mean[at] = r.mean;
+    rstd[at] = r.rstd;
+  });
+  __syncthreads();
+  float mu[kA], sc[kN], sh[kN];
+#pragma unroll
+  for (int j = 0; j < kN; ++j) {
+    const Stats r = st[(w.c + j) / d.Cg];
+    if (j < kA) mu[j] = r.mean;
+    sc[j] = r.rstd * ga[j];
+    sh[j] = __builtin_fmaf(-r.rest, sc[j], be[j]);
+  }
+  packed(raw);
+  const Buf ry = w.over(d, y);
+#pragma unroll
+  for (int i = 0; i < kR; ++i) {
+    if (!w.any(i)) continue;
+    auto v = vals_of<kType>(raw[i]);
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+      v.set(j, act_of<kAct>(__builtin_fmaf(v[j] - mu[kOne ? 0 : j], sc[j], sh[j])));
+    __builtin_amdgcn_raw_buffer_store_b128(raw_of<kType>(v), ry, w.at + i * w.step, 0, kAuxNT);
+  }
+}
+
+// dz is formed once and kept in fp32 beside x.  Grid: K N slabs workgroups.
+template <int kType, int kAct, int kR, bool kOne>
+__global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d, const void* __restrict__ dy,
+                                                      const void* __restrict__ x,
+                                                      const float* __restrict__ gamma,
+                                                      const float* __restrict__ beta, int64_t ld,
+                                                      const float* __restrict__ mean,
+                                                      const float* __restrict__ rstd,
+                                                      void* __restrict__ dx) {
+  constexpr int kN = Elem<kType>::kVec;
+  constexpr int kA = kOne ? 1 : kN;
+  const Held<kType, kR> w(d);
+  u32x4 raw[kR], rdy[kR];
+  w.load(w.over(d, x), raw);
+  w.load(w.over(d, dy), rdy);
+  const int t = (int)threadIdx.x;
+  float mu[kA], rs[kA], gs[kN], be[kN];
+  const int64_t g0 = w.n * d.G + w.c0 / d.Cg;
+#pragma unroll
+  for (int j = 0; j < kA; ++j) {
+    mu[j] = mean[g0 + (w.c + j) / d.Cg];
+    rs[j] = rstd[g0 + (w.c + j) / d.Cg];
+  }
+#pragma unroll
+  for (int j = 0; j < kN; ++j) {
+    gs[j] = gamma[w.k * ld + w.c0 + w.c + j] * rs[kOne ? 0 : j];
+    be[j] = beta[w.k * ld + w.c0 + w.c + j];
+  }
+  // per channel: sum of dz (x - mean), and of dz
+  float a[kN] = {}, b[kN] = {};
+  float dz[kR][kN];
+#pragma unroll
+  for (int i = 0; i < kR; ++i) {
+    if (!w.any(i)) continue;
+    const auto v = vals_of<kType>(raw[i]), g = vals_of<kType>(rdy[i]);
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      const float u = v[j] - mu[kOne ? 0 : j];
+      const float q = act_back<kAct>(g[j], __builtin_fmaf(u, gs[j], be[j]));
+      dz[i][j] = q;
+      a[j] = __builtin_fmaf(q, u, a[j]);
+      b[j] += q;
+    }
+  }
+  // element f of the threads' sums side by side belongs to channel f mod cw
+  const int cw = w.cols * kN, elems = w.active * kN;
+  float* ta = reinterpret_cast<float*>(dyn_lds);
+  float* tb = ta + (int)blockDim.x * kN;
+  double* ca = reinterpret_cast<double*>(tb + (int)blockDim.x * kN);  // [cw 2] channel sums
+  float2* sg = reinterpret_cast<float2*>(ca + 2 * cw);                // [groups] s1, s2
+  if (t < w.active) {
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      ta[t * kN + j] = a[j];
+      tb[t * kN + j] = b[j];
+    }
+  }
+  __syncthreads();
+  double* part = d.part + (w.n * d.C + w.c0) * 2;
+  for (int q = t; q < 2 * cw; q += (int)blockDim.x) {
+    const int c = q >= cw ? q - cw : q;
+    const float* p = q >= cw ? tb : ta;
+    double s = 0.0;
+    for (int f = c; f < elems; f += cw) s += (double)p[f];
+    if (q < cw) s *= (double)rstd[g0 + c / d.Cg];
+    part[2 * c + (q >= cw)] = s;
+    ca[2 * c + (q >= cw)] = s * (double)gamma[w.k * ld + w.c0 + c];
+  }
+  __syncthreads();
+  const double m = (double)d.P * d.Cg;
+  join_sums(cw / d.Cg, d.Cg, [&](int g, int i) {
+    return reinterpret_cast<const double2*>(ca)[g * d.Cg + i];
+  }, [&](int g, double2 s) { sg[g] = make_float2((float)(s.y / m), (float)(s.x / m)); });
+  __syncthreads();
+  // dx = gamma rstd dz - rstd s1 - (x - mean) rstd^2 s2
+  float k1[kA], k2[kA];
+#pragma unroll
+  for (int j = 0; j < kA; ++j) {
+    const float2 s = sg[(w.c + j) / d.Cg];
+    k1[j] = rs[j] * s.x;
+    k2[j] = rs[j] * rs[j] * s.y;
+  }
+  packed(raw);
+  const Buf ro = w.over(d, dx);
+#pragma unroll
+  for (int i = 0; i < kR; ++i) {
+    if (!w.any(i)) continue;
+    auto v = vals_of<kType>(raw[i]);
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      const int o = kOne ? 0 : j;
+      const float u = v[j] - mu[o];
+      v.set(j, __builtin_fmaf(gs[j], dz[i][j], -__builtin_fmaf(u, k2[o], k1[o])));
+    }
+    __builtin_amdgcn_raw_buffer_store_b128(raw_of<kType>(v), ro, w.at + i * w.step, 0, kAuxNT);
+  }
+}
+
+// dgamma and dbeta: the channel sums over a worker's samples and pixel ranges.
+// Grid: K ceil(C / 64) workgroups of 16 waves; wave w adds rows w, w + 16, ...
+constexpr int kParamWaves = 16;
+__global__ __launch_bounds__(kParamWaves* kWave) void k_gn_params(GroupNormDev d, int splits,
+                                                                  float* __restrict__ dgamma,
+                                                                  float* __restrict__ dbeta,
+                                                                  int64_t ldg) {
+  __shared__ double2 s_p[kParamWaves][kWave];
   const unsigned per = (unsigned)((d.C + kWave - 1) / kWave);
   const int k = (int)(blockIdx.x / per);
   const int c = (int)(blockIdx.x % per) * kWave + lane_id();
   const int w = wave_id();
-  const int64_t rows = d.N * d.splits;
-  double a = 0.0, b = 0.0;
+  const int64_t rows = d.N * splits;
+  double2 s = make_double2(0.0, 0.0);
   if (c < d.C) {
-    const double* p = d.part + (k * rows * d.C + c) * 2;
-    for (int64_t i = w; i < rows; i += kWaves) {
-      a += p[i * d.C * 2];
-      b += p[i * d.C * 2 + 1];
+    const double2* p = reinterpret_cast<const double2*>(d.part) + k * rows * d.C + c;
+#pragma unroll 4
+    for (int64_t i = w; i < rows; i += kParamWaves) {
+      const double2 v = p[i * d.C];
+      s.x += v.x;
+      s.y += v.y;
     }
   }
-  s_a[w][lane_id()] = a;
-  s_b[w][lane_id()] = b;
+  s_p[w][lane_id()] = s;
   __syncthreads();
   if (w != 0 || c >= d.C) return;
-  for (int i = 1; i < kWaves; ++i) {
-    a += s_a[i][lane_id()];
-    b += s_b[i][lane_id()];
+  for (int i = 1; i < kParamWaves; ++i) {
+    s.x += s_p[i][lane_id()].x;
+    s.y += s_p[i][lane_id()].y;
   }
-  dgamma[k * ldg + c] = (float)a;
-  dbeta[k * ldg + c] = (float)b;
+  dgamma[k * ldg + c] = (float)s.x;
+  dbeta[k * ldg + c] = (float)s.y;
 }
 
 // Calls f with the element type, the vector width and the activation as
@@ -395,42 +781,121 @@ hipError_t dispatch(int dtype, int vec, int act, F&& f) {
   return hipGetLastError();
 }
 
-// LDS of a workgroup: a value of each thread's elements, or the group sums.
-size_t sums_lds(const GroupNormDev& d, size_t bytes) { return (size_t)d.threads * d.vec * bytes; }
-size_t groups_lds(const GroupNormDev& d) { return ((size_t)d.slab / d.Cg + 2) * sizeof(GroupSums); }
+// The same for the one-pass kernels: f(type, act, vectors of a thread, one).
+template <typename F>
+hipError_t dispatch_held(int dtype, int act, int r, bool one, F&& f) {
+  auto with_one = [&](auto type, auto a, auto n) {
+    if (one) f(type, a, n, std::true_type());
+    else f(type, a, n, std::false_type());
+  };
+  auto with_r = [&](auto type, auto a) {
+    if (r == 16) with_one(type, a, std::integral_constant<int, 16>());
+    else if (r == 2) with_one(type, a, std::integral_constant<int, 2>());
+    else if (r == 4) with_one(type, a, std::integral_constant<int, 4>());
+    else with_one(type, a, std::integral_constant<int, 8>());
+  };
+  auto with_act = [&](auto type) {
+    if (act == kActRelu) with_r(type, std::integral_constant<int, kActRelu>());
+    else if (act == kActSilu) with_r(type, std::integral_constant<int, kActSilu>());
+    else with_r(type, std::integral_constant<int, kActNone>());
+  };
+  if (dtype == kF32) with_act(std::integral_constant<int, kF32>());
+  else if (dtype == kBF16) with_act(std::integral_constant<int, kBF16>());
+  else with_act(std::integral_constant<int, kF16>());
+  return hipGetLastError();
+}
+
+// Threads of a workgroup that lay their sums in LDS, at most (fold_lanes; the
+// last slab may be narrower than the others).
+int places(const GroupNormDev& d) {
+  auto of = [&](int cw) {
+    const int period = cw / std::min(d.vec, cw & -cw);
+    return period < kWave && (period & (period - 1)) == 0 ? kBlock / kWave * period : kBlock;
+  };
+  return std::max(of(d.slab), of(d.C - (d.slabs - 1) * d.slab));
+}
+
+bool aligned16(const void* a, const void* b, const void* c) {
+  return ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) |
+           reinterpret_cast<uintptr_t>(c)) & 15u) == 0;
+}
 
 }  // namespace
 
-hipError_t launch_group_norm_forward(const GroupNormDev& d, int dtype, int act, const void* x,
-                                     const float* gamma, const float* beta, int64_t ld, void* y,
-                                     float* mean, float* rstd, hipStream_t s) {
+hipError_t launch_group_norm_forward(const GroupNormDev& d, const GroupNormHeld& held, int dtype,
+                                     int act, const void* x, const float* gamma,
+                                     const float* beta, int64_t ld, void* y, float* mean,
+                                     float* rstd, hipStream_t s) {
   const LaunchEvents ev;
-  const dim3 grid((unsigned)(d.K * d.N * d.slabs * d.splits)), block((unsigned)d.threads);
+  if (held.threads > 0 && aligned16(x, y, nullptr)) {
+    GroupNormDev h = d;
+    h.slab = held.slab;
+    h.slabs = held.slabs;
+    const int vec = 16 / dtype_bytes(dtype);
+    const bool one = d.Cg % vec == 0;
+    const size_t lds = (size_t)held.threads * (one ? 1 : vec) * sizeof(double2) +
+                       (size_t)(held.slab / d.Cg) * sizeof(Stats);
+    const dim3 grid((unsigned)(d.K * d.N * h.slabs)), block((unsigned)held.threads);
+    return dispatch_held(dtype, act, held.vectors, one, [&](auto type, auto a, auto r, auto o) {
+      constexpr int T = decltype(type)::value, A = decltype(a)::value, R = decltype(r)::value;
+      constexpr bool O = decltype(o)::value;
+      SAEF_LAUNCH((k_gn_fwd_held<T, A, R, O>), grid, block, lds, s, h, x, gamma, beta, ld, y, mean,
+                  rstd);
+    });
+  }
+  const dim3 grid((unsigned)(d.K * d.N * d.slabs * d.splits)), block(kBlock);
+  const bool one = d.vec > 1 && d.C % d.vec == 0 && d.Cg % d.vec == 0;
+  const size_t lds = (size_t)places(d) * (one ? 1 : d.vec) * sizeof(double2);
+  const size_t stats = ((size_t)d.slab / d.Cg + 2) * sizeof(Stats);
   return dispatch(dtype, d.vec, act, [&](auto type, auto n, auto a) {
     constexpr int T = decltype(type)::value, V = decltype(n)::value, A = decltype(a)::value;
-    SAEF_LAUNCH((k_gn_sums<T, V, kActNone, false>), grid, block, sums_lds(d, sizeof(double)), s, d,
-                x, nullptr, nullptr, nullptr, ld, nullptr, nullptr);
-    SAEF_LAUNCH((k_gn_apply<T, V, A>), grid, block, groups_lds(d), s, d, x, gamma, beta, ld, y,
-                mean, rstd);
+    if (one) SAEF_LAUNCH((k_gn_fwd_sums<T, V, true>), grid, block, lds, s, d, x);
+    else SAEF_LAUNCH((k_gn_fwd_sums<T, V, false>), grid, block, lds, s, d, x);
+    SAEF_LAUNCH((k_gn_fwd_apply<T, V, A>), grid, block, stats, s, d, x, gamma, beta, ld, y, mean,
+                rstd);
   });
 }
 
-hipError_t launch_group_norm_backward(const GroupNormDev& d, int dtype, int act, const void* dy,
-                                      const void* x, const float* gamma, const float* beta,
-                                      int64_t ld, const float* mean, const float* rstd, void* dx,
-                                      float* dgamma, float* dbeta, int64_t ldg, hipStream_t s) {
+hipError_t launch_group_norm_backward(const GroupNormDev& d, const GroupNormHeld& held, int dtype,
+                                      int act, const void* dy, const void* x, const float* gamma,
+                                      const float* beta, int64_t ld, const float* mean,
+                                      const float* rstd, void* dx, float* dgamma, float* dbeta,
+                                      int64_t ldg, hipStream_t s) {
   const LaunchEvents ev;
-  const dim3 grid((unsigned)(d.K * d.N * d.slabs * d.splits)), block((unsigned)d.threads);
-  const hipError_t err = dispatch(dtype, d.vec, act, [&](auto type, auto n, auto a) {
-    constexpr int T = decltype(type)::value, V = decltype(n)::value, A = decltype(a)::value;
-    SAEF_LAUNCH((k_gn_sums<T, V, A, true>), grid, block, sums_lds(d, sizeof(float)), s, d, x, dy,
-                gamma, beta, ld, mean, rstd);
-    SAEF_LAUNCH((k_gn_back<T, V, A>), grid, block, groups_lds(d), s, d, dy, x, gamma, beta, ld,
-                mean, rstd, dx);
-  });
+  hipError_t err;
+  int splits = d.splits;
+  if (held.threads > 0 && aligned16(x, dy, dx)) {
+    GroupNormDev h = d;
+    h.slab = held.slab;
+    h.slabs = held.slabs;
+    splits = 1;
+    const int vec = 16 / dtype_bytes(dtype);
+    const bool one = d.Cg % vec == 0;
+    const size_t lds = (size_t)held.threads * vec * 2 * sizeof(float) +
+                       (size_t)held.slab * 2 * sizeof(double) +
+                       (size_t)(held.slab / d.Cg) * sizeof(float2);
+    const dim3 grid((unsigned)(d.K * d.N * h.slabs)), block((unsigned)held.threads);
+    err = dispatch_held(dtype, act, held.vectors, one, [&](auto type, auto a, auto r, auto o) {
+      constexpr int T = decltype(type)::value, A = decltype(a)::value, R = decltype(r)::value;
+      constexpr bool O = decltype(o)::value;
+      SAEF_LAUNCH((k_gn_bwd_held<T, A, R, O>), grid, block, lds, s, h, dy, x, gamma, beta, ld,
+                  mean, rstd, dx);
+    });
+  } else {
+    const dim3 grid((unsigned)(d.K * d.N * d.slabs * d.splits)), block(kBlock);
+    const size_t lds = (size_t)places(d) * d.vec * sizeof(float2) + (size_t)d.slab * sizeof(double2);
+    const size_t means = ((size_t)d.slab / d.Cg + 2) * sizeof(float2);
+    err = dispatch(dtype, d.vec, act, [&](auto type, auto n, auto a) {
+      constexpr int T = decltype(type)::value, V = decltype(n)::value, A = decltype(a)::value;
+      SAEF_LAUNCH((k_gn_bwd_sums<T, V, A>), grid, block, lds, s, d, x, dy, gamma, beta, ld, mean,
+                  rstd);
+      SAEF_LAUNCH((k_gn_bwd_apply<T, V, A>), grid, block, means, s, d, dy, x, gamma, beta, ld,
+                  mean, rstd, dx);
+    });
+  }
   if (err != hipSuccess) return err;
   const dim3 pgrid((unsigned)d.K * (unsigned)((d.C + kWave - 1) / kWave));
-  SAEF_LAUNCH(k_gn_params, pgrid, dim3(kBlock), 0, s, d, dgamma, dbeta, ldg);
+  SAEF_LAUNCH(k_gn_params, pgrid, dim3(kParamWaves * kWave), 0, s, d, splits, dgamma, dbeta, ldg);
   return hipGetLastError();
 }
 

@@ -131,8 +131,11 @@ def _w(t):
 
 
 def _stream(stream):
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    # torch.cuda.current_stream().cuda_stream without the Stream object in
+    # between: 0.4 us instead of 2.9 a call
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 class Layout:
@@ -351,6 +354,7 @@ class GroupNorm:
                                            ctypes.byref(handle)))
         self._h = handle
         self.K, self.N, self.P, self.C, self.G = K, N, P, C, G
+        self.numel, self.groups = K * N * P * C, K * N * G
         self.dtype = dtype
 
     @property
@@ -362,17 +366,17 @@ class GroupNorm:
     def _features(self, t, what):
         """Address of K N P C features: a contiguous tensor whose last dimension is
         C, or (K N, C, H, W) in torch's channels_last memory format."""
-        _sized(t, self.K * self.N * self.P * self.C, what)
-        if t.dim() == 4 and t.shape[:2] == (self.K * self.N, self.C) \
-                and t.is_contiguous(memory_format=torch.channels_last):
+        _sized(t, self.numel, what)
+        if t.dim() == 0 or t.shape[-1] != self.C or not t.is_contiguous():
+            if t.dim() != 4 or t.shape[:2] != (self.K * self.N, self.C) \
+                    or not t.is_contiguous(memory_format=torch.channels_last):
+                raise ValueError(f"{what} must be contiguous and channels last, C = {self.C}")
             t = t.permute(0, 2, 3, 1)
-        if t.shape[-1:] != (self.C,):
-            raise ValueError(f"{what} must be channels last, C = {self.C}")
         return _dev(t, self.dtype)
 
     def _params(self, t, what):
         """Address and worker stride of (K, C) values, contiguous along C."""
-        if tuple(t.shape) != (self.K, self.C):
+        if t.shape != (self.K, self.C):
             raise ValueError(f"{what} must be (K, C) = {(self.K, self.C)}, got {tuple(t.shape)}")
         if not t.is_cuda:
             raise TypeError("SAEF buffers must be device tensors")
@@ -405,7 +409,7 @@ def saef_group_norm_forward(plan: GroupNorm, x, gamma, beta, y, mean, rstd, stre
     of the evaluation points xh; mean, rstd (K, N, G) are written."""
     pg, pb, ld = plan._pair(gamma, beta, ("gamma", "beta"))
     for t, what in ((mean, "mean"), (rstd, "rstd")):
-        _sized(t, plan.K * plan.N * plan.G, what)
+        _sized(t, plan.groups, what)
     _check("saef_group_norm_forward",
            _lib.saef_group_norm_forward(plan.handle, plan._features(x, "x"), pg, pb, ld,
                                         plan._features(y, "y"), _f(mean), _f(rstd),
@@ -418,7 +422,7 @@ def saef_group_norm_backward(plan: GroupNorm, dy, x, gamma, beta, mean, rstd, dx
     pg, pb, ld = plan._pair(gamma, beta, ("gamma", "beta"))
     qg, qb, ldg = plan._pair(dgamma, dbeta, ("dgamma", "dbeta"))
     for t, what in ((mean, "mean"), (rstd, "rstd")):
-        _sized(t, plan.K * plan.N * plan.G, what)
+        _sized(t, plan.groups, what)
     _check("saef_group_norm_backward",
            _lib.saef_group_norm_backward(plan.handle, plan._features(dy, "dy"),
                                          plan._features(x, "x"), pg, pb, ld, _f(mean), _f(rstd),
