@@ -781,15 +781,23 @@ int saef_grads_create(const saef_layout* layout, int32_t K, int32_t dtype, void*
   g->K = K;
   g->dtype = dtype;
   hipError_t err = hipMalloc(&g->mem_ptr, rows * sizeof(void*));
-  if (err == hipSuccess)
-    err = hipMalloc(&g->mem_part, (size_t)K * layout->dev.n_tiles * sizeof(double));
+  // Runs of tiles: enough waves to fill the GPU a few times over (8 M tiles of 2^28 x
+  // 8 in runs of 32 1287 us, of 4 1356, one by one 1340; bert_base bf16 x 4 of 8
+  // 146, one by one 196).  A worker of few tiles has one workgroup, in one launch.
   const int64_t pairs = layout->dev.n_tiles * K;
+  const bool small = layout->dev.n_tiles <= saef::kSmallTiles;
   int32_t run_tiles = 1;
   while (run_tiles < 32 && pairs / run_tiles > 32768) run_tiles *= 2;
-  const int64_t runs = (layout->dev.n_tiles + run_tiles - 1) / run_tiles;
-  // What is read for the norm is read again to be clipped
+  const int64_t runs = small ? 0 : (layout->dev.n_tiles + run_tiles - 1) / run_tiles;
+  // What is read for the norm is read again to be clipped.  Up to 1 GB leaving it in
+  // the last-level cache pays over both (resnet56 x 8 15.1 us against 19.2, bert_base
+  // bf16 x 4 570 against 589, resnet50 x 8 394 both ways); beyond, loads that pass it
+  // by are faster (2^28 x 8: the norm 1290 against 1446).
   const int32_t cached = (double)K * layout->d_pad * es <= 1073741824.0;
-  if (err == hipSuccess) err = hipMalloc(&g->mem_runs, (size_t)K * runs * sizeof(double));
+  if (err == hipSuccess && !small)
+    err = hipMalloc(&g->mem_part, (size_t)K * layout->dev.n_tiles * sizeof(double));
+  if (err == hipSuccess && !small)
+    err = hipMalloc(&g->mem_runs, (size_t)K * runs * sizeof(double));
   if (err == hipSuccess)
     err = hipMemcpy(g->mem_ptr, ptr, rows * sizeof(void*), hipMemcpyHostToDevice);
   if (err != hipSuccess) {
@@ -1433,7 +1441,6 @@ saef::GroupNormHeld hold_group_norm(const saef::GroupNormDev& d, int dtype, bool
   const saef::GroupNormHeld none{0, 0, 0, 0};
   if (d.C % vec != 0 || d.P > (int64_t(1) << 31) / es / d.C - 1) return none;
   const int32_t unit = d.Cg / std::min(vec, d.Cg & -d.Cg) * vec;  // whole groups and vectors
-  const bool one = d.Cg % vec == 0;
   // Small workgroups first, then long rows; rows of less than 128 bytes only where
   // there are no more channels.
   for (int32_t most : {256, 512})
@@ -1445,10 +1452,9 @@ saef::GroupNormHeld hold_group_norm(const saef::GroupNormDev& d, int dtype, bool
       for (int32_t vectors : {2, 4, 8, 16}) {
         if (vectors == 16 && back) continue;  // (their values do not fit the registers)
         const int64_t threads = ((d.P + vectors - 1) / vectors * cols + 63) / 64 * 64;
-        const size_t lds = back ? (size_t)threads * vec * 8 + (size_t)slab * 24
-                                : (size_t)threads * (one ? 1 : vec) * 16 + (size_t)slab * 12;
-        if (threads > most || lds > 65536) continue;
-        return {(int32_t)threads, vectors, slab, (d.C + slab - 1) / slab};
+        if (threads > most) continue;
+        const saef::GroupNormHeld h{(int32_t)threads, vectors, slab, (d.C + slab - 1) / slab};
+        if (saef::group_norm_held_lds(d, h, dtype, back) <= saef::kMostLds) return h;
       }
     }
   return none;

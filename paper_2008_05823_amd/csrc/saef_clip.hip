@@ -70,7 +70,8 @@ struct Acc {
   }
 };
 
-constexpr int kFinWaves = 4;  // of a workgroup that joins sums
+constexpr int kFinWaves = 4;    // of a workgroup that joins sums
+constexpr int kSmallWaves = 16;  // of one that takes a worker's whole gradient
 
 constexpr int kGU = 8;  // 16-byte loads of a wave in flight
 
@@ -88,6 +89,29 @@ struct Run {
   }
 };
 
+// The wave's tile into acc.
+template <int kType, bool kInf, int kAux>
+__device__ __forceinline__ void add_tile(const Span<kType>& sp, Acc<kInf>& acc) {
+  typedef Elem<kType> E;
+  const int lane = lane_id();
+  const Buf b = sp.body();
+  for (int v0 = 0; v0 < sp.nvec; v0 += kGU * kWave) {
+    u32x4 raw[kGU];
+#pragma unroll
+    for (int u = 0; u < kGU; ++u)
+      raw[u] = __builtin_amdgcn_raw_buffer_load_b128(b, (v0 + u * kWave + lane) * 16, 0, kAux);
+#pragma unroll
+    for (int u = 0; u < kGU; ++u) {
+      typename E::T v[E::kVec];
+      __builtin_memcpy(v, &raw[u], 16);
+#pragma unroll
+      for (int j = 0; j < E::kVec; ++j) acc.add(E::to_f32(v[j]));
+    }
+  }
+  if (lane < sp.head) acc.add(E::to_f32(sp.p[lane]));
+  if (lane < sp.tail) acc.add(E::to_f32(sp.tail_at()[lane]));
+}
+
 // A wave adds up its run tile by tile.  The run's sum goes to runs[k][run]; where
 // tensor sums are asked for, the part of each tensor in the run goes to the slot
 // of its first tile there.
@@ -95,30 +119,13 @@ template <int kType, bool kInf, bool kTensors, int kAux>
 __global__ __launch_bounds__(kBlock) void k_grad_tiles(DevLayout lay, GradsDev g) {
   const Run r(lay, g, blockIdx.x);
   if (r.first >= lay.n_tiles) return;
-  typedef Elem<kType> E;
   const int lane = lane_id();
   Acc<kInf> all, part;
   Tile tile = lay.tiles[r.first];
   int64_t slot = r.first;
   for (int64_t ti = r.first; ti < r.last; ++ti) {
     const Tile next = lay.tiles[min(ti + 1, lay.n_tiles - 1)];
-    const Span<kType> sp(lay, g, r.k, tile);
-    const Buf b = sp.body();
-    for (int v0 = 0; v0 < sp.nvec; v0 += kGU * kWave) {
-      u32x4 raw[kGU];
-#pragma unroll
-      for (int u = 0; u < kGU; ++u)
-        raw[u] = __builtin_amdgcn_raw_buffer_load_b128(b, (v0 + u * kWave + lane) * 16, 0, kAux);
-#pragma unroll
-      for (int u = 0; u < kGU; ++u) {
-        typename E::T v[E::kVec];
-        __builtin_memcpy(v, &raw[u], 16);
-#pragma unroll
-        for (int j = 0; j < E::kVec; ++j) part.add(E::to_f32(v[j]));
-      }
-    }
-    if (lane < sp.head) part.add(E::to_f32(sp.p[lane]));
-    if (lane < sp.tail) part.add(E::to_f32(sp.tail_at()[lane]));
+    add_tile<kType, kInf, kAux>(Span<kType>(lay, g, r.k, tile), part);
     if (kTensors && (next.l != tile.l || ti + 1 == r.last)) {
       all.join(part);
       const double s = part.wave();
@@ -139,18 +146,18 @@ __device__ __forceinline__ double joined(double p, double q) {
 }
 
 // The sum (or the largest) of at(0 .. n-1) over the workgroup, in thread 0.
-template <bool kInf, typename At>
+template <bool kInf, int kW, typename At>
 __device__ double block_join(int64_t n, At at) {
-  __shared__ double s_v[kFinWaves];
+  __shared__ double s_v[kW];
   double a = 0.0;
 #pragma unroll 4
-  for (int64_t i = threadIdx.x; i < n; i += kFinWaves * kWave) a = joined<kInf>(a, at(i));
+  for (int64_t i = threadIdx.x; i < n; i += kW * kWave) a = joined<kInf>(a, at(i));
 #pragma unroll
   for (int o = kWave / 2; o > 0; o >>= 1) a = joined<kInf>(a, __shfl_xor(a, o));
   if (lane_id() == 0) s_v[wave_id()] = a;
   __syncthreads();
   if (threadIdx.x == 0)
-    for (int i = 1; i < kFinWaves; ++i) a = joined<kInf>(a, s_v[i]);
+    for (int i = 1; i < kW; ++i) a = joined<kInf>(a, s_v[i]);
   return a;
 }
 
@@ -166,7 +173,7 @@ __global__ __launch_bounds__(kFinWaves* kWave) void k_grad_norms(
     DevLayout lay, GradsDev g, float* __restrict__ norms, float* __restrict__ tensor_norms) {
   if (blockIdx.x < (unsigned)g.K) {
     const double* v = g.run_sums + (int64_t)blockIdx.x * g.runs;
-    const double s = block_join<kInf>(g.runs, [&](int64_t i) { return v[i]; });
+    const double s = block_join<kInf, kFinWaves>(g.runs, [&](int64_t i) { return v[i]; });
     if (threadIdx.x == 0) norms[blockIdx.x] = norm_of<kInf>(s);
     return;
   }
@@ -176,9 +183,36 @@ __global__ __launch_bounds__(kFinWaves* kWave) void k_grad_norms(
   // the tensor's slots: its first tile, and those where a run begins
   const int64_t first = t.first_tile, run = first / g.run_tiles;
   const int64_t n = (first + t.ntiles - 1) / g.run_tiles - run + 1;
-  const double s = block_join<kInf>(
+  const double s = block_join<kInf, kFinWaves>(
       n, [&](int64_t i) { return v[i == 0 ? first : (run + i) * g.run_tiles]; });
   if (threadIdx.x == 0) tensor_norms[b] = norm_of<kInf>(s);
+}
+
+// Small gradients in one launch: a workgroup takes a worker's, its waves tile by
+// tile, and joins the tiles' sums from LDS.  Grid: K.
+template <int kType, bool kInf>
+__global__ __launch_bounds__(kSmallWaves* kWave) void k_grad_small(
+    DevLayout lay, GradsDev g, float* __restrict__ norms, float* __restrict__ tensor_norms) {
+  __shared__ double s_tile[kSmallTiles];
+  const int k = (int)blockIdx.x;
+  for (int ti = wave_id(); ti < (int)lay.n_tiles; ti += kSmallWaves) {
+    Acc<kInf> acc;
+    add_tile<kType, kInf, 0>(Span<kType>(lay, g, k, lay.tiles[ti]), acc);
+    const double s = acc.wave();
+    if (lane_id() == 0) s_tile[ti] = s;
+  }
+  __syncthreads();
+  if (tensor_norms != nullptr) {
+    for (int l = (int)threadIdx.x; l < lay.L; l += kSmallWaves * kWave) {
+      const TensorInfo t = lay.tensors[l];
+      double a = 0.0;
+      for (int i = 0; i < t.ntiles; ++i) a = joined<kInf>(a, s_tile[t.first_tile + i]);
+      tensor_norms[(int64_t)k * lay.L + l] = norm_of<kInf>(a);
+    }
+  }
+  const double s =
+      block_join<kInf, kSmallWaves>(lay.n_tiles, [&](int64_t i) { return s_tile[i]; });
+  if (threadIdx.x == 0) norms[k] = norm_of<kInf>(s);
 }
 
 // c v in the gradient's own type.  The product is rounded to fp32 first, in every
@@ -271,6 +305,16 @@ dim3 run_grid(const GradsDev& g) {
 hipError_t launch_grad_norm(const DevLayout& lay, const GradsDev& g, bool inf, float* norms,
                             float* tensor_norms, hipStream_t s) {
   const LaunchEvents ev;
+  if (g.runs == 0) {
+#define SAEF_GN(T, I)                                                                          \
+  SAEF_LAUNCH((k_grad_small<T, I>), dim3((unsigned)g.K), dim3(kSmallWaves * kWave), 0, s, lay, g, \
+              norms, tensor_norms)
+    if (g.dtype == kF32) { if (inf) SAEF_GN(kF32, true); else SAEF_GN(kF32, false); }
+    else if (g.dtype == kBF16) { if (inf) SAEF_GN(kBF16, true); else SAEF_GN(kBF16, false); }
+    else { if (inf) SAEF_GN(kF16, true); else SAEF_GN(kF16, false); }
+#undef SAEF_GN
+    return hipGetLastError();
+  }
   const dim3 runs = run_grid(g);
   const dim3 fin((unsigned)g.K * (tensor_norms != nullptr ? 1u + (unsigned)lay.L : 1u));
   const bool tensors = tensor_norms != nullptr;

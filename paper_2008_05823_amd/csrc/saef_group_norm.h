@@ -32,6 +32,11 @@ struct GroupNormHeld {
   int32_t threads, vectors, slab, slabs;
 };
 
+// LDS of such a workgroup; at most 64 KB may be asked for.
+size_t group_norm_held_lds(const GroupNormDev& d, const GroupNormHeld& held, int dtype,
+                           bool back);
+constexpr size_t kMostLds = 65536;
+
 hipError_t launch_group_norm_forward(const GroupNormDev& d, const GroupNormHeld& held, int dtype,
                                      int act, const void* x, const float* gamma,
                                      const float* beta, int64_t ld, void* y, float* mean,

@@ -129,12 +129,13 @@ __device__ __forceinline__ void join_sums(int count, int terms, At at, Put put) 
 
 // Before a workgroup's threads lay their sums side by side in LDS: where the
 // channels repeat every `period` threads, a power of two below a wave, the lanes
-// of a wave that share theirs are added first.  The return value is this
-// thread's place in the table, or -1, and `active` becomes the places.
+// of a wave that share theirs are added first.
+__host__ __device__ inline bool folds(int period) {
+  return period < kWave && (period & (period - 1)) == 0;
+}
 template <int kA, typename V>
-__device__ __forceinline__ int fold_lanes(V (&v)[kA], V (&w)[kA], int period, int& active) {
-  const int t = (int)threadIdx.x;
-  if (period >= kWave || (period & (period - 1)) != 0) return t < active ? t : -1;
+__device__ __forceinline__ void fold_lanes(V (&v)[kA], V (&w)[kA], int period) {
+  if (!folds(period)) return;
   for (int o = kWave / 2; o >= period; o /= 2) {
 #pragma unroll
     for (int j = 0; j < kA; ++j) {
@@ -142,9 +143,19 @@ __device__ __forceinline__ int fold_lanes(V (&v)[kA], V (&w)[kA], int period, in
       w[j] += __shfl_xor(w[j], o);
     }
   }
-  active = (int)blockDim.x / kWave * period;
+}
+// This thread's place in the table, or -1; `places`, the threads with sums,
+// becomes the number of places.
+__device__ __forceinline__ int fold_place(int period, int& places) {
+  const int t = (int)threadIdx.x;
+  if (!folds(period)) return t < places ? t : -1;
+  places = (int)blockDim.x / kWave * period;
   const int l = t % kWave;
   return l < period ? t / kWave * period + l : -1;
+}
+// Places of a workgroup of `threads` threads, at most.
+inline int table_places(int threads, int period) {
+  return folds(period) ? threads / kWave * period : threads;
 }
 
 // ------------------------------------------------------------------ two passes
@@ -310,16 +321,17 @@ __global__ __launch_bounds__(kBlock) void k_gn_fwd_sums(GroupNormDev d,
     }
   });
   double2* table = reinterpret_cast<double2*>(dyn_lds);
-  int active = w.active;
-  const int t = fold_lanes(a0, a1, w.period, active);
-  if (t >= 0) {
+  int places = w.active;
+  const int place = fold_place(w.period, places);
+  fold_lanes(a0, a1, w.period);
+  if (place >= 0) {
 #pragma unroll
-    for (int j = 0; j < kA; ++j) table[t * kA + j] = make_double2(a0[j], a1[j]);
+    for (int j = 0; j < kA; ++j) table[place * kA + j] = make_double2(a0[j], a1[j]);
   }
   __syncthreads();
   // entries of a pixel of the slab, and pixels
   constexpr int kPer = kN / kA;
-  const int wide = w.cw / kPer, rows = active * kA / wide, most = min(d.Cg, w.cw) / kPer;
+  const int wide = w.cw / kPer, rows = places * kA / wide, most = min(d.Cg, w.cw) / kPer;
   double2* out = reinterpret_cast<double2*>(d.pieces) +
                  (w.n * d.splits + w.s) * (d.G + d.slabs - 1) + w.group0(d) + w.b;
   join_sums(w.groups(d), rows * most, [&](int i, int q) {
@@ -403,9 +415,10 @@ __global__ __launch_bounds__(kBlock) void k_gn_bwd_sums(GroupNormDev d,
   }
   // element f of the threads' sums side by side belongs to channel f mod cw
   float2* table = reinterpret_cast<float2*>(dyn_lds);
-  int active = w.active;
-  const int place = fold_lanes(a, b, w.period, active);
-  const int t = (int)threadIdx.x, elems = active * kN;
+  int places = w.active;
+  const int place = fold_place(w.period, places);
+  fold_lanes(a, b, w.period);
+  const int t = (int)threadIdx.x, elems = places * kN;
   double2* sums = reinterpret_cast<double2*>(table + elems);
   if (place >= 0) {
 #pragma unroll
@@ -491,26 +504,24 @@ template <int kType, int kR>
 struct Held {
   static constexpr int kN = Elem<kType>::kVec;
   typedef typename Elem<kType>::T T;
-  int64_t n;        // sample, over all workers
-  int k, c0, c;     // worker, first channel of the slab and of the thread within it
-  int col, cols;    // the thread's column of vectors, and columns of the slab
-  int active;       // threads whose vectors make up whole pixels
-  uint32_t at;      // byte offset of the thread's first vector in the sample
-  uint32_t step;    // and to its next
-  uint32_t bytes;   // of the sample
+  int64_t n;       // sample, over all workers
+  int k, c0, c;    // worker, first channel of the slab and of the thread within it
+  int cols;        // columns of vectors in the slab
+  int active;      // threads whose vectors make up whole pixels
+  uint32_t at;     // byte offset of the thread's first vector in the sample
+  uint32_t step;   // and to its next
+  uint32_t bytes;  // of the sample
 
   __device__ __forceinline__ explicit Held(const GroupNormDev& d) {
-    const int b = (int)blockIdx.x;
-    c0 = b % d.slabs * d.slab;
-    n = b / d.slabs;
-    k = (int)(n / d.N);
+    c0 = (int)(blockIdx.x % (uint32_t)d.slabs) * d.slab;
+    n = blockIdx.x / (uint32_t)d.slabs;
+    k = (int)((uint32_t)n / (uint32_t)d.N);
     cols = min(d.slab, d.C - c0) / kN;
     const int t = (int)threadIdx.x;
     const int rows = (int)blockDim.x / cols;
     active = rows * cols;
     const int p = t / cols;
-    col = t - p * cols;
-    c = col * kN;
+    c = (t - p * cols) * kN;
     bytes = (uint32_t)d.P * (uint32_t)d.C * (uint32_t)sizeof(T);
     step = (uint32_t)rows * (uint32_t)d.C * (uint32_t)sizeof(T);
     at = t < active ? ((uint32_t)p * (uint32_t)d.C + (uint32_t)(c0 + c)) * (uint32_t)sizeof(T)
@@ -526,6 +537,7 @@ struct Held {
     for (int i = 0; i < kR; ++i)
       raw[i] = __builtin_amdgcn_raw_buffer_load_b128(r, at + i * step, 0, kAuxNT);
   }
+  __device__ __forceinline__ int groups(const GroupNormDev& d) const { return cols * kN / d.Cg; }
 };
 
 template <int kType>
@@ -556,24 +568,33 @@ __device__ __forceinline__ void packed(u32x4 (&raw)[kR]) {
 
 // kOne: a vector lies in one group.  Grid: K N slabs workgroups.
 template <int kType, int kAct, int kR, bool kOne>
-__global__ __launch_bounds__(kHeldThreads) void k_gn_fwd_held(GroupNormDev d, const void* __restrict__ x,
-                                                      const float* __restrict__ gamma,
-                                                      const float* __restrict__ beta, int64_t ld,
-                                                      void* __restrict__ y,
-                                                      float* __restrict__ mean,
-                                                      float* __restrict__ rstd) {
+__global__ __launch_bounds__(kHeldThreads) void k_gn_fwd_held(GroupNormDev d,
+                                                              const void* __restrict__ x,
+                                                              const float* __restrict__ gamma,
+                                                              const float* __restrict__ beta,
+                                                              int64_t ld, void* __restrict__ y,
+                                                              float* __restrict__ mean,
+                                                              float* __restrict__ rstd) {
   constexpr int kN = Elem<kType>::kVec;
   constexpr int kA = kOne ? 1 : kN;  // sums of a thread
   const Held<kType, kR> w(d);
   u32x4 raw[kR];
   w.load(w.over(d, x), raw);
-  const int t = (int)threadIdx.x;
   float ga[kN], be[kN];
 #pragma unroll
   for (int j = 0; j < kN; ++j) {
     ga[j] = gamma[w.k * ld + w.c0 + w.c + j];
     be[j] = beta[w.k * ld + w.c0 + w.c + j];
   }
+  // entry p kA + j of the table belongs to channel ((p kA + j) mod (cols kA)) kN / kA
+  double2* table = reinterpret_cast<double2*>(dyn_lds);
+  int places = w.active;
+  const int place = fold_place(w.cols, places);
+  Stats* st = reinterpret_cast<Stats*>(table + places * kA);
+  const int groups = w.groups(d);
+  const int wide = d.Cg * kA / kN;           // entries of a group in a pixel
+  const int terms = places / w.cols * wide;  // and in all
+  const double m = (double)d.P * d.Cg;
   double a0[kA] = {}, a1[kA] = {};
 #pragma unroll
   for (int i = 0; i < kR; ++i) {
@@ -586,20 +607,14 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_fwd_held(GroupNormDev d, co
       a1[kOne ? 0 : j] = __builtin_fma(f, f, a1[kOne ? 0 : j]);
     }
   }
-  // entry t kA + j of the table belongs to channel ((t kA + j) mod (cols kA)) kN / kA
-  double2* table = reinterpret_cast<double2*>(dyn_lds);
-  Stats* st = reinterpret_cast<Stats*>(table + (int)blockDim.x * kA);
-  if (t < w.active) {
+  fold_lanes(a0, a1, w.cols);
+  if (place >= 0) {
 #pragma unroll
-    for (int j = 0; j < kA; ++j) table[t * kA + j] = make_double2(a0[j], a1[j]);
+    for (int j = 0; j < kA; ++j) table[place * kA + j] = make_double2(a0[j], a1[j]);
   }
   __syncthreads();
-  const int groups = w.cols * kN / d.Cg;
-  const int wide = d.Cg * kA / kN;             // entries of a group in a pixel
-  const int terms = w.active / w.cols * wide;  // and in all
-  const double m = (double)d.P * d.Cg;
-  join_sums(groups, terms, [&](int g, int q) {
-    return table[q / wide * w.cols * kA + g * wide + q % wide];
+  join_sums(groups, terms, [&](int g, int e) {
+    return table[e / wide * w.cols * kA + g * wide + e % wide];
   }, [&](int g, double2 s) {
     const Stats r = stats_of(s.x, s.y, m, d.eps);
     st[g] = r;
@@ -631,13 +646,15 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_fwd_held(GroupNormDev d, co
 
 // dz is formed once and kept in fp32 beside x.  Grid: K N slabs workgroups.
 template <int kType, int kAct, int kR, bool kOne>
-__global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d, const void* __restrict__ dy,
-                                                      const void* __restrict__ x,
-                                                      const float* __restrict__ gamma,
-                                                      const float* __restrict__ beta, int64_t ld,
-                                                      const float* __restrict__ mean,
-                                                      const float* __restrict__ rstd,
-                                                      void* __restrict__ dx) {
+__global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d,
+                                                              const void* __restrict__ dy,
+                                                              const void* __restrict__ x,
+                                                              const float* __restrict__ gamma,
+                                                              const float* __restrict__ beta,
+                                                              int64_t ld,
+                                                              const float* __restrict__ mean,
+                                                              const float* __restrict__ rstd,
+                                                              void* __restrict__ dx) {
   constexpr int kN = Elem<kType>::kVec;
   constexpr int kA = kOne ? 1 : kN;
   const Held<kType, kR> w(d);
@@ -657,6 +674,14 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d, co
     gs[j] = gamma[w.k * ld + w.c0 + w.c + j] * rs[kOne ? 0 : j];
     be[j] = beta[w.k * ld + w.c0 + w.c + j];
   }
+  int places = w.active;
+  const int place = fold_place(w.cols, places);
+  const int cw = w.cols * kN, elems = places * kN, groups = w.groups(d);
+  float* ta = reinterpret_cast<float*>(dyn_lds);
+  float* tb = ta + elems;
+  double* ca = reinterpret_cast<double*>(tb + elems);   // [cw 2] channel sums
+  float2* sg = reinterpret_cast<float2*>(ca + 2 * cw);  // [groups] s1, s2
+  const double m = (double)d.P * d.Cg;
   // per channel: sum of dz (x - mean), and of dz
   float a[kN] = {}, b[kN] = {};
   float dz[kR][kN];
@@ -674,32 +699,27 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d, co
     }
   }
   // element f of the threads' sums side by side belongs to channel f mod cw
-  const int cw = w.cols * kN, elems = w.active * kN;
-  float* ta = reinterpret_cast<float*>(dyn_lds);
-  float* tb = ta + (int)blockDim.x * kN;
-  double* ca = reinterpret_cast<double*>(tb + (int)blockDim.x * kN);  // [cw 2] channel sums
-  float2* sg = reinterpret_cast<float2*>(ca + 2 * cw);                // [groups] s1, s2
-  if (t < w.active) {
+  fold_lanes(a, b, w.cols);
+  if (place >= 0) {
 #pragma unroll
     for (int j = 0; j < kN; ++j) {
-      ta[t * kN + j] = a[j];
-      tb[t * kN + j] = b[j];
+      ta[place * kN + j] = a[j];
+      tb[place * kN + j] = b[j];
     }
   }
   __syncthreads();
   double* part = d.part + (w.n * d.C + w.c0) * 2;
-  for (int q = t; q < 2 * cw; q += (int)blockDim.x) {
-    const int c = q >= cw ? q - cw : q;
-    const float* p = q >= cw ? tb : ta;
+  for (int e = t; e < 2 * cw; e += (int)blockDim.x) {
+    const int c = e >= cw ? e - cw : e;
+    const float* p = e >= cw ? tb : ta;
     double s = 0.0;
     for (int f = c; f < elems; f += cw) s += (double)p[f];
-    if (q < cw) s *= (double)rstd[g0 + c / d.Cg];
-    part[2 * c + (q >= cw)] = s;
-    ca[2 * c + (q >= cw)] = s * (double)gamma[w.k * ld + w.c0 + c];
+    if (e < cw) s *= (double)rstd[g0 + c / d.Cg];
+    part[2 * c + (e >= cw)] = s;
+    ca[2 * c + (e >= cw)] = s * (double)gamma[w.k * ld + w.c0 + c];
   }
   __syncthreads();
-  const double m = (double)d.P * d.Cg;
-  join_sums(cw / d.Cg, d.Cg, [&](int g, int i) {
+  join_sums(groups, d.Cg, [&](int g, int i) {
     return reinterpret_cast<const double2*>(ca)[g * d.Cg + i];
   }, [&](int g, double2 s) { sg[g] = make_float2((float)(s.y / m), (float)(s.x / m)); });
   __syncthreads();
@@ -790,9 +810,9 @@ hipError_t dispatch_held(int dtype, int act, int r, bool one, F&& f) {
   };
   auto with_r = [&](auto type, auto a) {
     if (r == 16) with_one(type, a, std::integral_constant<int, 16>());
-    else if (r == 2) with_one(type, a, std::integral_constant<int, 2>());
+    else if (r == 8) with_one(type, a, std::integral_constant<int, 8>());
     else if (r == 4) with_one(type, a, std::integral_constant<int, 4>());
-    else with_one(type, a, std::integral_constant<int, 8>());
+    else with_one(type, a, std::integral_constant<int, 2>());
   };
   auto with_act = [&](auto type) {
     if (act == kActRelu) with_r(type, std::integral_constant<int, kActRelu>());
@@ -805,13 +825,10 @@ hipError_t dispatch_held(int dtype, int act, int r, bool one, F&& f) {
   return hipGetLastError();
 }
 
-// Threads of a workgroup that lay their sums in LDS, at most (fold_lanes; the
-// last slab may be narrower than the others).
+// Places in LDS of the two-pass sums (the last slab may be narrower than the
+// others).
 int places(const GroupNormDev& d) {
-  auto of = [&](int cw) {
-    const int period = cw / std::min(d.vec, cw & -cw);
-    return period < kWave && (period & (period - 1)) == 0 ? kBlock / kWave * period : kBlock;
-  };
+  auto of = [&](int cw) { return table_places(kBlock, cw / std::min(d.vec, cw & -cw)); };
   return std::max(of(d.slab), of(d.C - (d.slabs - 1) * d.slab));
 }
 
@@ -822,6 +839,18 @@ bool aligned16(const void* a, const void* b, const void* c) {
 
 }  // namespace
 
+size_t group_norm_held_lds(const GroupNormDev& d, const GroupNormHeld& held, int dtype,
+                           bool back) {
+  const int vec = 16 / dtype_bytes(dtype), groups = held.slab / d.Cg;
+  const int last = d.C - (held.slabs - 1) * held.slab;  // channels of the last slab
+  const size_t at = (size_t)std::max(table_places(held.threads, held.slab / vec),
+                                     table_places(held.threads, last / vec));
+  if (back)
+    return at * vec * 2 * sizeof(float) + (size_t)held.slab * 2 * sizeof(double) +
+           groups * sizeof(float2);
+  return at * (d.Cg % vec == 0 ? 1 : vec) * sizeof(double2) + groups * sizeof(Stats);
+}
+
 hipError_t launch_group_norm_forward(const GroupNormDev& d, const GroupNormHeld& held, int dtype,
                                      int act, const void* x, const float* gamma,
                                      const float* beta, int64_t ld, void* y, float* mean,
@@ -831,10 +860,8 @@ hipError_t launch_group_norm_forward(const GroupNormDev& d, const GroupNormHeld&
     GroupNormDev h = d;
     h.slab = held.slab;
     h.slabs = held.slabs;
-    const int vec = 16 / dtype_bytes(dtype);
-    const bool one = d.Cg % vec == 0;
-    const size_t lds = (size_t)held.threads * (one ? 1 : vec) * sizeof(double2) +
-                       (size_t)(held.slab / d.Cg) * sizeof(Stats);
+    const bool one = d.Cg % (16 / dtype_bytes(dtype)) == 0;
+    const size_t lds = group_norm_held_lds(d, held, dtype, false);
     const dim3 grid((unsigned)(d.K * d.N * h.slabs)), block((unsigned)held.threads);
     return dispatch_held(dtype, act, held.vectors, one, [&](auto type, auto a, auto r, auto o) {
       constexpr int T = decltype(type)::value, A = decltype(a)::value, R = decltype(r)::value;
@@ -869,17 +896,15 @@ hipError_t launch_group_norm_backward(const GroupNormDev& d, const GroupNormHeld
     h.slab = held.slab;
     h.slabs = held.slabs;
     splits = 1;
-    const int vec = 16 / dtype_bytes(dtype);
-    const bool one = d.Cg % vec == 0;
-    const size_t lds = (size_t)held.threads * vec * 2 * sizeof(float) +
-                       (size_t)held.slab * 2 * sizeof(double) +
-                       (size_t)(held.slab / d.Cg) * sizeof(float2);
+    const bool one = d.Cg % (16 / dtype_bytes(dtype)) == 0;
+    const size_t lds = group_norm_held_lds(d, held, dtype, true);
     const dim3 grid((unsigned)(d.K * d.N * h.slabs)), block((unsigned)held.threads);
     err = dispatch_held(dtype, act, held.vectors, one, [&](auto type, auto a, auto r, auto o) {
       constexpr int T = decltype(type)::value, A = decltype(a)::value, R = decltype(r)::value;
       constexpr bool O = decltype(o)::value;
-      SAEF_LAUNCH((k_gn_bwd_held<T, A, R, O>), grid, block, lds, s, h, dy, x, gamma, beta, ld,
-                  mean, rstd, dx);
+      if constexpr (R <= 8)  // (16 do not fit the registers and are never chosen)
+        SAEF_LAUNCH((k_gn_bwd_held<T, A, R, O>), grid, block, lds, s, h, dy, x, gamma, beta, ld,
+                    mean, rstd, dx);
     });
   } else {
     const dim3 grid((unsigned)(d.K * d.N * d.slabs * d.splits)), block(kBlock);

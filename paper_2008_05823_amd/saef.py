@@ -355,6 +355,7 @@ class GroupNorm:
         self._h = handle
         self.K, self.N, self.P, self.C, self.G = K, N, P, C, G
         self.numel, self.groups = K * N * P * C, K * N * G
+        self.param_shape = torch.Size((K, C))
         self.dtype = dtype
 
     @property
@@ -366,7 +367,10 @@ class GroupNorm:
     def _features(self, t, what):
         """Address of K N P C features: a contiguous tensor whose last dimension is
         C, or (K N, C, H, W) in torch's channels_last memory format."""
-        _sized(t, self.numel, what)
+        if t.dtype == self.dtype and t.is_cuda and t.numel() == self.numel and t.dim() > 0 \
+                and t.shape[-1] == self.C and t.is_contiguous():
+            return t.data_ptr()
+        _sized(t, self.numel, what)  # else: the other layout, or why not
         if t.dim() == 0 or t.shape[-1] != self.C or not t.is_contiguous():
             if t.dim() != 4 or t.shape[:2] != (self.K * self.N, self.C) \
                     or not t.is_contiguous(memory_format=torch.channels_last):
@@ -376,6 +380,10 @@ class GroupNorm:
 
     def _params(self, t, what):
         """Address and worker stride of (K, C) values, contiguous along C."""
+        if t.dtype == torch.float32 and t.is_cuda and t.shape == self.param_shape:
+            a, b = t.stride()
+            if b == 1:
+                return t.data_ptr(), a if self.K > 1 else self.C
         if t.shape != (self.K, self.C):
             raise ValueError(f"{what} must be (K, C) = {(self.K, self.C)}, got {tuple(t.shape)}")
         if not t.is_cuda:
@@ -408,8 +416,8 @@ def saef_group_norm_forward(plan: GroupNorm, x, gamma, beta, y, mean, rstd, stre
     """y = act(gamma (x - mean) rstd + beta); gamma, beta (K, C), e.g. columns
     of the evaluation points xh; mean, rstd (K, N, G) are written."""
     pg, pb, ld = plan._pair(gamma, beta, ("gamma", "beta"))
-    for t, what in ((mean, "mean"), (rstd, "rstd")):
-        _sized(t, plan.groups, what)
+    _sized(mean, plan.groups, "mean")
+    _sized(rstd, plan.groups, "rstd")
     _check("saef_group_norm_forward",
            _lib.saef_group_norm_forward(plan.handle, plan._features(x, "x"), pg, pb, ld,
                                         plan._features(y, "y"), _f(mean), _f(rstd),
@@ -421,8 +429,8 @@ def saef_group_norm_backward(plan: GroupNorm, dy, x, gamma, beta, mean, rstd, dx
     """dx, and dgamma, dbeta (K, C), e.g. columns of the gradient rows g."""
     pg, pb, ld = plan._pair(gamma, beta, ("gamma", "beta"))
     qg, qb, ldg = plan._pair(dgamma, dbeta, ("dgamma", "dbeta"))
-    for t, what in ((mean, "mean"), (rstd, "rstd")):
-        _sized(t, plan.groups, what)
+    _sized(mean, plan.groups, "mean")
+    _sized(rstd, plan.groups, "rstd")
     _check("saef_group_norm_backward",
            _lib.saef_group_norm_backward(plan.handle, plan._features(dy, "dy"),
                                          plan._features(x, "x"), pg, pb, ld, _f(mean), _f(rstd),
