@@ -8,6 +8,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -46,11 +47,25 @@ def hipcc() -> str:
 def build(out: str = LIB, verbose: bool = False, defines=()) -> str:
     """Compile the library to `out`; `defines` are extra -D options (tuning
     variants, e.g. SAEF_TILE_ELEMS=2048)."""
-    cmd = [hipcc(), *HIPCC_FLAGS, *[f"-D{d}" for d in defines],
-           "-I", os.path.join(ROOT, "include"), "-o", out + ".tmp", *SOURCES]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"] + [f"-D{d}" for d in defines]
+    with tempfile.TemporaryDirectory() as tmp:
+        # the sources side by side, then one link
+        runs, objects = [], []
+        for src in SOURCES:
+            objects.append(os.path.join(tmp, os.path.basename(src) + ".o"))
+            cmd = [hipcc(), *flags, "-I", os.path.join(ROOT, "include"), "-c", src, "-o",
+                   objects[-1]]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            runs.append(subprocess.Popen(cmd, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE,
+                                         text=True))
+        stderr = "".join([r.communicate()[1] for r in runs])
+        res = subprocess.CompletedProcess([], max(abs(r.returncode) for r in runs), stderr=stderr)
+        if res.returncode == 0:
+            link = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", out + ".tmp",
+                    *objects]
+            res = subprocess.run(link, capture_output=True, text=True)
+            res.stderr = stderr + res.stderr
     # the host pass does not know the packed-fp32 feature and says so; harmless
     noise = [ln for ln in res.stderr.splitlines() if "packed-fp32-ops" not in ln
              and "warning generated" not in ln and ln.strip()]

@@ -1449,7 +1449,7 @@ saef::GroupNormHeld hold_group_norm(const saef::GroupNormDev& d, int dtype, bool
       // a pixel or few: wider slabs
       while (slab < d.C && d.P * slab < 512 * vec) slab = std::min(d.C, 2 * slab);
       const int32_t cols = slab / vec;
-      for (int32_t vectors : {2, 4, 8, 16}) {
+      for (int32_t vectors : {4, 8, 16}) {
         if (vectors == 16 && back) continue;  // (their values do not fit the registers)
         const int64_t threads = ((d.P + vectors - 1) / vectors * cols + 63) / 64 * 64;
         if (threads > most) continue;

@@ -811,8 +811,7 @@ hipError_t dispatch_held(int dtype, int act, int r, bool one, F&& f) {
   auto with_r = [&](auto type, auto a) {
     if (r == 16) with_one(type, a, std::integral_constant<int, 16>());
     else if (r == 8) with_one(type, a, std::integral_constant<int, 8>());
-    else if (r == 4) with_one(type, a, std::integral_constant<int, 4>());
-    else with_one(type, a, std::integral_constant<int, 2>());
+    else with_one(type, a, std::integral_constant<int, 4>());
   };
   auto with_act = [&](auto type) {
     if (act == kActRelu) with_r(type, std::integral_constant<int, kActRelu>());
