@@ -83,18 +83,18 @@ __device__ __forceinline__ float act_back(float dy, float z) {
   return dy;
 }
 
-// The statistics of m values from their sum and sum of squares.
+// The statistics of m values from their sum and sum of squares; inv_m = 1 / m.
 struct Stats {
   float mean, rest, rstd;  // mean rounded to fp32, and what that leaves
 };
-__device__ __forceinline__ Stats stats_of(double s0, double s1, double m, float eps) {
-  const double mu = s0 / m;
-  const double var = s1 / m - mu * mu;
+__device__ __forceinline__ Stats stats_of(double s0, double s1, double inv_m, float eps) {
+  const double mu = s0 * inv_m;
+  const double var = s1 * inv_m - mu * mu;
   Stats r;
   r.mean = (float)mu;
   r.rest = (float)(mu - (double)r.mean);
   // (a rounding below 0 is 0; what is no number stays none)
-  r.rstd = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)eps));
+  r.rstd = (float)rsqrt((var < 0.0 ? 0.0 : var) + (double)eps);
   return r;
 }
 
@@ -353,9 +353,14 @@ __global__ __launch_bounds__(kBlock) void k_gn_fwd_apply(GroupNormDev d,
   Stream<kType, kN, 1> in(w, x);
   Stats* st = reinterpret_cast<Stats*>(dyn_lds);
   const int g0 = w.group0(d);
-  const double m = (double)d.P * d.Cg;
+  float mu[kN], sc[kN], sh[kN];
+  w.channels(d, [&](int j, int c, int) {
+    sc[j] = gamma[w.k * ld + c];
+    sh[j] = beta[w.k * ld + c];
+  });
+  const double inv_m = 1.0 / ((double)d.P * d.Cg);
   join_groups(d, w, [&](int i, double2 s) {
-    const Stats r = stats_of(s.x, s.y, m, d.eps);
+    const Stats r = stats_of(s.x, s.y, inv_m, d.eps);
     st[i] = r;
     // (a group in several slabs: all write the same)
     if (w.s == 0) {
@@ -365,12 +370,11 @@ __global__ __launch_bounds__(kBlock) void k_gn_fwd_apply(GroupNormDev d,
   });
   __syncthreads();
   if (w.left <= 0) return;
-  float mu[kN], sc[kN], sh[kN];
-  w.channels(d, [&](int j, int c, int g) {
+  w.channels(d, [&](int j, int, int g) {
     const Stats r = st[g - g0];
     mu[j] = r.mean;
-    sc[j] = r.rstd * gamma[w.k * ld + c];
-    sh[j] = __builtin_fmaf(-r.rest, sc[j], beta[w.k * ld + c]);
+    sc[j] = r.rstd * sc[j];
+    sh[j] = __builtin_fmaf(-r.rest, sc[j], sh[j]);
   });
   in.each([&](Vals<kType, kN>* v, int64_t at, int n) {
 #pragma unroll
@@ -462,21 +466,23 @@ __global__ __launch_bounds__(kBlock) void k_gn_bwd_apply(GroupNormDev d,
   Stream<kType, kN, 2> in(w, x, dy);
   float2* st = reinterpret_cast<float2*>(dyn_lds);
   const int g0 = w.group0(d);
-  const double m = (double)d.P * d.Cg;
+  float mu[kN], gs[kN], be[kN], k1[kN], k2[kN];
+  w.channels(d, [&](int j, int c, int g) {
+    mu[j] = mean[w.n * d.G + g];
+    k1[j] = rstd[w.n * d.G + g];
+    gs[j] = gamma[w.k * ld + c] * k1[j];
+    be[j] = beta[w.k * ld + c];
+  });
+  const double inv_m = 1.0 / ((double)d.P * d.Cg);
   join_groups(d, w, [&](int i, double2 s) {
-    st[i] = make_float2((float)(s.y / m), (float)(s.x / m));
+    st[i] = make_float2((float)(s.y * inv_m), (float)(s.x * inv_m));
   });
   __syncthreads();
   if (w.left <= 0) return;
   // dx = gamma rstd dz - rstd s1 - (x - mean) rstd^2 s2
-  float mu[kN], gs[kN], be[kN], k1[kN], k2[kN];
-  w.channels(d, [&](int j, int c, int g) {
-    const float r = rstd[w.n * d.G + g];
-    mu[j] = mean[w.n * d.G + g];
-    gs[j] = gamma[w.k * ld + c] * r;
-    be[j] = beta[w.k * ld + c];
-    k1[j] = r * st[g - g0].x;
-    k2[j] = r * r * st[g - g0].y;
+  w.channels(d, [&](int j, int, int g) {
+    k2[j] = k1[j] * k1[j] * st[g - g0].y;
+    k1[j] *= st[g - g0].x;
   });
   in.each([&](Vals<kType, kN>* v, int64_t at, int n) {
 #pragma unroll
@@ -594,7 +600,7 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_fwd_held(GroupNormDev d,
   const int groups = w.groups(d);
   const int wide = d.Cg * kA / kN;           // entries of a group in a pixel
   const int terms = places / w.cols * wide;  // and in all
-  const double m = (double)d.P * d.Cg;
+  const double inv_m = 1.0 / ((double)d.P * d.Cg);
   double a0[kA] = {}, a1[kA] = {};
 #pragma unroll
   for (int i = 0; i < kR; ++i) {
@@ -616,7 +622,7 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_fwd_held(GroupNormDev d,
   join_sums(groups, terms, [&](int g, int e) {
     return table[e / wide * w.cols * kA + g * wide + e % wide];
   }, [&](int g, double2 s) {
-    const Stats r = stats_of(s.x, s.y, m, d.eps);
+    const Stats r = stats_of(s.x, s.y, inv_m, d.eps);
     st[g] = r;
     const int64_t at = w.n * d.G + w.c0 / d.Cg + g;
     mean[at] = r.mean;
@@ -681,7 +687,7 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d,
   float* tb = ta + elems;
   double* ca = reinterpret_cast<double*>(tb + elems);   // [cw 2] channel sums
   float2* sg = reinterpret_cast<float2*>(ca + 2 * cw);  // [groups] s1, s2
-  const double m = (double)d.P * d.Cg;
+  const double inv_m = 1.0 / ((double)d.P * d.Cg);
   // per channel: sum of dz (x - mean), and of dz
   float a[kN] = {}, b[kN] = {};
   float dz[kR][kN];
@@ -698,6 +704,11 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d,
       b[j] += q;
     }
   }
+  // (what this thread's channel sum is scaled by, on its way before the barrier)
+  const int c1 = t < cw ? t : t - cw;
+  const bool sums = t < 2 * cw;
+  const float r1 = sums ? rstd[g0 + c1 / d.Cg] : 0.0f;
+  const float ga1 = sums ? gamma[w.k * ld + w.c0 + c1] : 0.0f;
   // element f of the threads' sums side by side belongs to channel f mod cw
   fold_lanes(a, b, w.cols);
   if (place >= 0) {
@@ -714,14 +725,16 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d,
     const float* p = e >= cw ? tb : ta;
     double s = 0.0;
     for (int f = c; f < elems; f += cw) s += (double)p[f];
-    if (e < cw) s *= (double)rstd[g0 + c / d.Cg];
+    const float r = e == t ? r1 : rstd[g0 + c / d.Cg];
+    const float ga = e == t ? ga1 : gamma[w.k * ld + w.c0 + c];
+    if (e < cw) s *= (double)r;
     part[2 * c + (e >= cw)] = s;
-    ca[2 * c + (e >= cw)] = s * (double)gamma[w.k * ld + w.c0 + c];
+    ca[2 * c + (e >= cw)] = s * (double)ga;
   }
   __syncthreads();
   join_sums(groups, d.Cg, [&](int g, int i) {
     return reinterpret_cast<const double2*>(ca)[g * d.Cg + i];
-  }, [&](int g, double2 s) { sg[g] = make_float2((float)(s.y / m), (float)(s.x / m)); });
+  }, [&](int g, double2 s) { sg[g] = make_float2((float)(s.y * inv_m), (float)(s.x * inv_m)); });
   __syncthreads();
   // dx = gamma rstd dz - rstd s1 - (x - mean) rstd^2 s2
   float k1[kA], k2[kA];
@@ -748,7 +761,7 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d,
 }
 
 // dgamma and dbeta: the channel sums over a worker's samples and pixel ranges.
-// Grid: K ceil(C / 64) workgroups of 16 waves; wave w adds rows w, w + 16, ...
+// Grid: K ceil(C / 64) workgroups of up to 16 waves, which take the rows in turn.
 constexpr int kParamWaves = 16;
 __global__ __launch_bounds__(kParamWaves* kWave) void k_gn_params(GroupNormDev d, int splits,
                                                                   float* __restrict__ dgamma,
@@ -756,7 +769,7 @@ __global__ __launch_bounds__(kParamWaves* kWave) void k_gn_params(GroupNormDev d
                                                                   int64_t ldg) {
   __shared__ double2 s_p[kParamWaves][kWave];
   const unsigned per = (unsigned)((d.C + kWave - 1) / kWave);
-  const int k = (int)(blockIdx.x / per);
+  const int k = (int)(blockIdx.x / per), waves = (int)blockDim.x / kWave;
   const int c = (int)(blockIdx.x % per) * kWave + lane_id();
   const int w = wave_id();
   const int64_t rows = d.N * splits;
@@ -764,7 +777,7 @@ __global__ __launch_bounds__(kParamWaves* kWave) void k_gn_params(GroupNormDev d
   if (c < d.C) {
     const double2* p = reinterpret_cast<const double2*>(d.part) + k * rows * d.C + c;
 #pragma unroll 4
-    for (int64_t i = w; i < rows; i += kParamWaves) {
+    for (int64_t i = w; i < rows; i += waves) {
       const double2 v = p[i * d.C];
       s.x += v.x;
       s.y += v.y;
@@ -773,7 +786,7 @@ __global__ __launch_bounds__(kParamWaves* kWave) void k_gn_params(GroupNormDev d
   s_p[w][lane_id()] = s;
   __syncthreads();
   if (w != 0 || c >= d.C) return;
-  for (int i = 1; i < kParamWaves; ++i) {
+  for (int i = 1; i < waves; ++i) {
     s.x += s_p[i][lane_id()].x;
     s.y += s_p[i][lane_id()].y;
   }
@@ -919,7 +932,9 @@ hipError_t launch_group_norm_backward(const GroupNormDev& d, const GroupNormHeld
   }
   if (err != hipSuccess) return err;
   const dim3 pgrid((unsigned)d.K * (unsigned)((d.C + kWave - 1) / kWave));
-  SAEF_LAUNCH(k_gn_params, pgrid, dim3(kParamWaves * kWave), 0, s, d, splits, dgamma, dbeta, ldg);
+  // four rows a wave, on their way together
+  const int waves = (int)std::min<int64_t>(kParamWaves, (d.N * splits + 3) / 4);
+  SAEF_LAUNCH(k_gn_params, pgrid, dim3((unsigned)(waves * kWave)), 0, s, d, splits, dgamma, dbeta, ldg);
   return hipGetLastError();
 }
 
