@@ -35,14 +35,22 @@ struct Vals {
   typedef typename Elem<kType>::T T;
   T v[kN];
   __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(v, p, sizeof(v)); }
+  // 16 bytes at the alignment of the smallest element
+  typedef unsigned int Raw __attribute__((ext_vector_type(4), aligned(2)));
+  __device__ __forceinline__ void load_nt(const T* p) {
+    if constexpr (sizeof(v) == 16) {
+      const Raw r = __builtin_nontemporal_load(reinterpret_cast<const Raw*>(p));
+      __builtin_memcpy(v, &r, 16);
+    } else {
+      load(p);
+    }
+  }
   __device__ __forceinline__ void load(const T* p, int n) {
 #pragma unroll
     for (int j = 0; j < kN; ++j) v[j] = j < n ? p[j] : (T)0.0f;
   }
   __device__ __forceinline__ void store(T* p) const {
     if constexpr (sizeof(v) == 16) {
-      // 16 bytes at the alignment of the smallest element
-      typedef unsigned int Raw __attribute__((ext_vector_type(4), aligned(2)));
       Raw r;
       __builtin_memcpy(&r, v, 16);
       __builtin_nontemporal_store(r, reinterpret_cast<Raw*>(p));
@@ -234,8 +242,10 @@ struct Part {
 };
 
 // The vectors of a thread's part, from kS features at once: kU of each are on
-// their way while the kU before are used.
-template <int kType, int kN, int kS>
+// their way while the kU before are used.  kLast: nobody reads them again, so they pass
+// the last-level cache by (784 x 512 bf16, 256 samples, backward 190 us, 206 without;
+// in the first pass the same costs: 50 MB forward 25 us instead of 20).
+template <int kType, int kN, int kS, bool kLast>
 struct Stream {
   typedef typename Elem<kType>::T T;
   const T* src[kS];
@@ -255,7 +265,10 @@ struct Stream {
     for (int u = 0; u < kU; ++u) {
       const int64_t p = left - u * dec >= kN ? from + u * stride : from;
 #pragma unroll
-      for (int i = 0; i < kS; ++i) to[u][i].load(src[i] + p);
+      for (int i = 0; i < kS; ++i) {
+        if (kLast) to[u][i].load_nt(src[i] + p);
+        else to[u][i].load(src[i] + p);
+      }
     }
   }
   // Calls f(v, at, n) with the thread's vectors one after another: n elements
@@ -312,7 +325,7 @@ __global__ __launch_bounds__(kBlock) void k_gn_fwd_sums(GroupNormDev d,
   constexpr int kA = kOne ? 1 : kN;  // sums of a thread
   const Part<kN> w(d, blockIdx.x);
   double a0[kA] = {}, a1[kA] = {};
-  Stream<kType, kN, 1>(w, x).each([&](Vals<kType, kN>* v, int64_t, int) {
+  Stream<kType, kN, 1, false>(w, x).each([&](Vals<kType, kN>* v, int64_t, int) {
 #pragma unroll
     for (int j = 0; j < kN; ++j) {
       const double f = v[0][j];
@@ -350,7 +363,7 @@ __global__ __launch_bounds__(kBlock) void k_gn_fwd_apply(GroupNormDev d,
                                                          float* __restrict__ rstd) {
   typedef typename Elem<kType>::T T;
   const Part<kN> w(d, d.backwards ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-  Stream<kType, kN, 1> in(w, x);
+  Stream<kType, kN, 1, true> in(w, x);
   Stats* st = reinterpret_cast<Stats*>(dyn_lds);
   const int g0 = w.group0(d);
   float mu[kN], sc[kN], sh[kN];
@@ -396,7 +409,7 @@ __global__ __launch_bounds__(kBlock) void k_gn_bwd_sums(GroupNormDev d,
                                                         const float* __restrict__ mean,
                                                         const float* __restrict__ rstd) {
   const Part<kN> w(d, blockIdx.x);
-  Stream<kType, kN, 2> in(w, x, dy);
+  Stream<kType, kN, 2, false> in(w, x, dy);
   float a[kN] = {}, b[kN] = {};
   if (w.left > 0) {
     float mu[kN], gs[kN], be[kN];
@@ -463,7 +476,7 @@ __global__ __launch_bounds__(kBlock) void k_gn_bwd_apply(GroupNormDev d,
                                                          void* __restrict__ dx) {
   typedef typename Elem<kType>::T T;
   const Part<kN> w(d, d.backwards ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-  Stream<kType, kN, 2> in(w, x, dy);
+  Stream<kType, kN, 2, true> in(w, x, dy);
   float2* st = reinterpret_cast<float2*>(dyn_lds);
   const int g0 = w.group0(d);
   float mu[kN], gs[kN], be[kN], k1[kN], k2[kN];

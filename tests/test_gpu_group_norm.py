@@ -294,3 +294,36 @@ def test_another_stream_and_graph_replays(shape):
         graph.replay()
         for p, q in zip(want, results()):
             assert torch.equal(p, q), i
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("shape", [(2, 2, 49, 64, 8), (1, 2, 3136, 64, 8), (1, 1, 65, 30, 5)], ids=str)
+def test_features_at_odd_addresses(shape, dtype):
+    """Features that start one element past an alignment boundary, as slices of larger
+    buffers do: aligned ones may be read another way, so the results agree to rounding."""
+    S = _S()
+    K, N, P, C, G = shape
+    x, dy, gamma, beta = _inputs(shape, dtype, 10)
+    n = x.numel()
+
+    def odd(t=None):
+        buf = torch.full((n + 9,), -5.0, dtype=DT[dtype], device="cuda")
+        v = buf[1:n + 1].view(x.shape)
+        if t is not None:
+            v.copy_(t)
+        return buf, v
+    (_, xo), (_, dyo), (ybuf, yo), (dbuf, dxo) = odd(x), odd(dy), odd(), odd()
+    plan = _plan(S, shape, dtype, "silu")
+    mean, rstd = (torch.empty((K, N, G), device="cuda") for _ in range(2))
+    S.saef_group_norm_forward(plan, xo, gamma, beta, yo, mean, rstd)
+    _check_forward(_np(x), _np(gamma), _np(beta), G, "silu", dtype, yo, mean, rstd)
+    dg, db = torch.empty((K, C), device="cuda"), torch.empty((K, C), device="cuda")
+    S.saef_group_norm_backward(plan, dyo, xo, gamma, beta, mean, rstd, dxo, dg, db)
+    (wx, wg, wb), (ex, eg, eb) = O.backward(_np(dy), _np(x), _np(mean), _np(rstd), _np(gamma),
+                                            _np(beta), "silu")
+    rel, tiny = O.OUT[dtype]
+    O.assert_within(_np(dxo), wx, ex + rel * (np.abs(wx) + ex) + tiny, "dx")
+    O.assert_within(_np(dg), wg, eg + O.U * np.abs(wg), "dgamma")
+    O.assert_within(_np(db), wb, eb + O.U * np.abs(wb), "dbeta")
+    for buf in (ybuf, dbuf):  # nothing around them is written
+        assert float(buf[0]) == -5.0 and bool((buf[n + 1:] == -5.0).all())
