@@ -228,10 +228,10 @@ int saef_materialize(const saef_layout* layout, int32_t K, int32_t mode, const f
  * for parameters in the rows of xh (C contiguous values, ld >= C).
  * Statistics are formed in binary64, the rest in fp32; y is rounded once, to
  * dtype.  mean, rstd: (K, N, G), for the backward pass.
- * A group norm is planned for one shape; the plan owns 16 bytes of device
- * scratch per channel, sample and pixel range (saef_group_norm_create chooses how many
- * of those a sample is cut into).  Calls that use one plan must not run
- * concurrently.  K <= 4096, C <= 65536, G divides C, eps > 0. */
+ * A group norm is planned for one shape; the plan owns at most 24 bytes of
+ * device scratch per channel, sample and pixel range (one range per 2048 to 8192
+ * loads of a sample).  Calls that use one plan must not run concurrently.
+ *  K <= 4096, C <= 65536, G divides C, eps > 0. */
 typedef struct saef_group_norm saef_group_norm;
 
 int saef_group_norm_create(int32_t K, int64_t N, int64_t P, int32_t C, int32_t G, int32_t dtype,
@@ -272,8 +272,8 @@ int saef_group_norm_backward(const saef_group_norm* plan, const void* dy, const 
  * of worker k, of type dtype, aligned to an element: a row of the layout at
  * off[l], a tensor that automatic differentiation filled, or a piece of a
  * bucket.  No two may overlap; the memory must stay while the handle is
- * used.  The handle owns 8 bytes of device scratch per (tile, worker), and
- * per (tensor, worker) 16.  Calls that use one saef_grads must not run
+ * used.  The handle owns device scratch: 8 bytes per (tensor, worker), and up
+ * to 16 per (tile, worker).  Calls that use one saef_grads must not run
  * concurrently.  Synchronous; the layout must outlive the handle. */
 typedef struct saef_grads saef_grads;
 

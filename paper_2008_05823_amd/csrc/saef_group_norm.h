@@ -21,7 +21,7 @@ struct GroupNormDev {
   int32_t slabs;   // ceil(C / slab)
   int32_t splits;  // workgroups over the pixels of a sample
   int32_t backwards;  // the second pass goes through the samples backwards
-  double* part;    // [K N splits C 2] backward sums per channel
+  float* part;     // [K N splits C 2] backward sums per channel
   double* pieces;  // [K N splits (G + slabs - 1) 2] sums per group and slab
 };
 

