@@ -754,6 +754,11 @@ int saef_grads_create(const saef_layout* layout, int32_t K, int32_t dtype, void*
   int rc = check_common(layout, K);
   if (rc != SAEF_OK) return rc;
   if (ptr == nullptr || dtype < SAEF_F32 || dtype > SAEF_F16) return SAEF_EINVAL;
+  // a launch has at most 2^32 - 1 threads: a wave per (tile, worker), a workgroup per
+  // (tensor, worker) and one per worker
+  if ((double)K * (layout->dev.n_tiles + saef::kWaves) * saef::kWave >= 4294967296.0 ||
+      (double)K * (layout->L + 1.0) * saef::kBlock >= 4294967296.0)
+    return SAEF_EINVAL;
   const size_t es = (size_t)saef::dtype_bytes(dtype);
   const size_t rows = (size_t)K * layout->L;
   saef_grads* g = nullptr;
@@ -1474,6 +1479,17 @@ GnSizes gn_sizes(const saef_group_norm* p, int64_t ld) {
           ((size_t)(d.K - 1) * ld + d.C) * sizeof(float), (size_t)d.K * d.N * d.G * sizeof(float)};
 }
 
+// A row of a (K rows of C values, ld apart) shares memory with one of b?  They may
+// lie in one another's gaps.
+bool rows_meet(const saef_group_norm* p, const float* a, const float* b, int64_t ld) {
+  const size_t bytes = gn_sizes(p, ld).params;
+  if (!overlap(a, bytes, b, bytes)) return false;
+  const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
+  const uintptr_t row = (uintptr_t)p->dev.C * sizeof(float), step = (uintptr_t)ld * sizeof(float);
+  const uintptr_t apart = (pa < pb ? pb - pa : pa - pb) % step;
+  return apart < row || apart > step - row;
+}
+
 int check_group_norm(const saef_group_norm* p) {
   if (p == nullptr) return SAEF_EINVAL;
   int dev = -1;
@@ -1579,14 +1595,13 @@ int saef_group_norm_backward(const saef_group_norm* plan, const void* dy, const 
   if (ld < plan->dev.C || ld > most || ldg < plan->dev.C || ldg > most) return SAEF_EINVAL;
   const GnSizes z = gn_sizes(plan, ld);
   const size_t gb = gn_sizes(plan, ldg).params;
-  // rows of the two parameters may lie in one another's gaps
-  const size_t row = (size_t)plan->dev.C * sizeof(float);
   const Range in[6] = {{dy, z.features},  {x, z.features}, {gamma, z.params},
                        {beta, z.params}, {mean, z.stats}, {rstd, z.stats}};
   for (const Range& r : in)
     if (overlap_any(r.p, r.bytes, {{dx, z.features}, {dgamma, gb}, {dbeta, gb}}))
       return SAEF_EINVAL;
-  if (overlap_any(dx, z.features, {{dgamma, gb}, {dbeta, gb}}) || overlap(dgamma, row, dbeta, row))
+  if (overlap_any(dx, z.features, {{dgamma, gb}, {dbeta, gb}}) ||
+      rows_meet(plan, dgamma, dbeta, ldg))
     return SAEF_EINVAL;
   return hip_rc(saef::launch_group_norm_backward(plan->dev, plan->bwd, plan->dtype, plan->act, dy,
                                                  x, gamma, beta, ld, mean, rstd, dx, dgamma,

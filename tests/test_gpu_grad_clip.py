@@ -1,4 +1,5 @@
 """Gradient norms, clipping and the clipped second half of an iteration on the GPU."""
+import ctypes
 import math
 
 import numpy as np
@@ -402,3 +403,17 @@ def test_another_stream_and_graph_replays():
                     mask[o:o + m] = True
                 same = same[:, mask]
             assert bool(same.all()), i
+
+
+def test_more_tensors_than_a_launch_takes_is_refused():
+    """4096 workers of 4200 one-element tensors: 17.2 M (tensor, worker) pairs, a workgroup
+    of 256 threads each, are more threads than a launch may have."""
+    S = _S()
+    L, K = 4200, 4096
+    lay = S.Layout([64 * i for i in range(L)], [1] * L, 64 * L, K)
+    base = torch.zeros(L * K, device="cuda")
+    p = base.data_ptr()
+    table = (ctypes.c_void_p * (L * K))(*range(p, p + 4 * L * K, 4))
+    handle = ctypes.c_void_p()
+    rc = S.raw_library().saef_grads_create(lay.handle, K, 0, table, ctypes.byref(handle))
+    assert rc == S.EINVAL and handle.value is None

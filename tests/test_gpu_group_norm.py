@@ -245,6 +245,13 @@ def test_channels_last_tensors_and_refusals():
     back(S.SaefError, x, dg[:, :16], dg[:, 16:32])
     back(S.SaefError, y, dg[:, :16], dg[:, 16:32])
     back(S.SaefError, dx, dg[:, :16], dg[:, 8:24])
+    # dbeta of one worker over dgamma of the next
+    tall = torch.zeros((3, 64), device="cuda")
+    back(S.SaefError, dx, tall[:2, :16], tall[1:, :16])
+    back(S.SaefError, dx, tall[1:, :16], tall[:2, 8:24])
+    back(S.SaefError, dx, tall[:2, 56:].as_strided((2, 16), (64, 1)), tall[1:, :16])
+    S.saef_group_norm_backward(plan, y, x, gamma, beta, mean, rstd, dx, tall[:2, 48:],
+                               tall[1:, :16])
     back(S.SaefError, dx, gamma, beta)
     back(ValueError, dx, dg[:, :16], dg[:1, 16:32])
     plan.destroy()
