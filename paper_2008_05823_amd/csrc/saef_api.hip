@@ -1437,6 +1437,7 @@ void cut_group_norm(saef::GroupNormDev& d, int dtype) {
   const int64_t items = (int64_t)d.K * d.N * d.slabs, round = (int64_t)saef::kBlock * d.vec;
   const int64_t most = d.P * d.slab / (round * 8), least = d.P * d.slab / (round * 32) + 1;
   d.splits = (int32_t)std::max(least, std::min((wgs + items - 1) / items, most));
+  d.split_pixels = (d.P + d.splits - 1) / d.splits;
   d.backwards = (double)d.K * d.N * d.P * d.C * saef::dtype_bytes(dtype) > 268435456.0;
 }
 

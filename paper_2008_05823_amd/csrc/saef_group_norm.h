@@ -20,6 +20,7 @@ struct GroupNormDev {
   int32_t slab;    // channels of a workgroup: C, or a multiple of vec
   int32_t slabs;   // ceil(C / slab)
   int32_t splits;  // workgroups over the pixels of a sample
+  int64_t split_pixels;  // pixels of each
   int32_t backwards;  // the second pass goes through the samples backwards
   float* part;     // [K N splits C 2] backward sums per channel
   double* pieces;  // [K N splits (G + slabs - 1) 2] sums per group and slab

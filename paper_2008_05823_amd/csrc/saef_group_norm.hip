@@ -199,8 +199,7 @@ struct Part {
     n = item / (uint32_t)d.slabs;
     k = (int)((uint32_t)n / (uint32_t)d.N);
     cw = min(d.slab, d.C - c0);
-    const int64_t per = (d.P + d.splits - 1) / d.splits;
-    const int64_t p0 = min(d.P, s * per), p1 = min(d.P, p0 + per);
+    const int64_t p0 = min(d.P, s * d.split_pixels), p1 = min(d.P, p0 + d.split_pixels);
     // threads whose elements make up whole pixels of the slab
     period = cw / min(kN, cw & -cw);
     active = (int)blockDim.x / period * period;
@@ -210,8 +209,8 @@ struct Part {
     c = f - p * cw;
     first = (n * d.P + p0 + p) * d.C + c0 + c;
     left = t < active ? (p1 - p0) * cw - f : 0;
-    dec = (int64_t)active * kN;
-    stride = dec / cw * d.C;
+    dec = active * kN;
+    stride = (int64_t)(active * kN / cw) * d.C;
   }
   // Calls f(j, channel, group) for the thread's elements j.
   template <typename F>
@@ -315,6 +314,11 @@ __device__ __forceinline__ void join_groups(const GroupNormDev& d, const Part<kN
   // slabs a group may lie in, at most
   const int span = d.slab % d.Cg == 0 ? 1 : min(d.slabs, (d.Cg - 1) / d.slab + 2);
   const double2* pieces = reinterpret_cast<const double2*>(d.pieces) + w.n * d.splits * Q;
+  if (span == 1) {  // whole groups: those of this slab
+    pieces += w.group0(d) + w.b;
+    join_sums(w.groups(d), d.splits, [&](int i, int q) { return pieces[(int64_t)q * Q + i]; }, put);
+    return;
+  }
   join_sums(w.groups(d), d.splits * span, [&](int i, int q) {
     const int g = w.group0(d) + i, b = g * d.Cg / d.slab + q % span;
     if (b > (g * d.Cg + d.Cg - 1) / d.slab) return make_double2(0.0, 0.0);
