@@ -26,6 +26,8 @@ struct GroupNormDev {
   double* pieces;  // [K N splits (G + slabs - 1) 2] sums per group and slab
 };
 
+constexpr int kParamWaves = 16;  // of a workgroup that adds up 64 channels of dgamma and dbeta
+
 // How a kernel that reads its features once cuts the work: workgroups of
 // `threads` threads, each holding `vectors` 16-byte vectors, take slabs of
 // `slab` channels of whole groups.  threads == 0: the shape does not fit.

@@ -444,7 +444,7 @@ __global__ __launch_bounds__(kBlock) void k_gn_bwd_sums(GroupNormDev d,
   const int place = fold_place(w.period, places);
   fold_lanes(a, b, w.period);
   const int t = (int)threadIdx.x, elems = places * kN;
-  double2* sums = reinterpret_cast<double2*>(table + elems);
+  double2* sums = reinterpret_cast<double2*>(table + (elems + 1) / 2 * 2);  // 16-byte aligned
   if (place >= 0) {
 #pragma unroll
     for (int j = 0; j < kN; ++j) table[place * kN + j] = make_float2(a[j], b[j]);
@@ -784,8 +784,7 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d,
 // dgamma and dbeta: the channel sums over a worker's samples and pixel ranges, which
 // are kept in fp32 (with a pixel or few a sample they are as large as the features) and
 // added up in binary64.
-// Grid: K ceil(C / 64) workgroups of up to 16 waves, which take the rows in turn.
-constexpr int kParamWaves = 16;
+// Grid: K ceil(C / 64) workgroups of up to kParamWaves waves, which take the rows in turn.
 __global__ __launch_bounds__(kParamWaves* kWave) void k_gn_params(GroupNormDev d, int splits,
                                                                   float* __restrict__ dgamma,
                                                                   float* __restrict__ dbeta,
@@ -944,7 +943,8 @@ hipError_t launch_group_norm_backward(const GroupNormDev& d, const GroupNormHeld
     });
   } else {
     const dim3 grid((unsigned)(d.K * d.N * d.slabs * d.splits)), block(kBlock);
-    const size_t lds = (size_t)places(d) * d.vec * sizeof(float2) + (size_t)d.slab * sizeof(double2);
+    const size_t lds = ((size_t)places(d) * d.vec + 1) * sizeof(float2) +
+                       (size_t)d.slab * sizeof(double2);
     const size_t means = ((size_t)d.slab / d.Cg + 2) * sizeof(float2);
     err = dispatch(dtype, d.vec, act, [&](auto type, auto n, auto a) {
       constexpr int T = decltype(type)::value, V = decltype(n)::value, A = decltype(a)::value;
@@ -958,7 +958,8 @@ hipError_t launch_group_norm_backward(const GroupNormDev& d, const GroupNormHeld
   const dim3 pgrid((unsigned)d.K * (unsigned)((d.C + kWave - 1) / kWave));
   // four rows a wave, on their way together
   const int waves = (int)std::min<int64_t>(kParamWaves, (d.N * splits + 3) / 4);
-  SAEF_LAUNCH(k_gn_params, pgrid, dim3((unsigned)(waves * kWave)), 0, s, d, splits, dgamma, dbeta, ldg);
+  SAEF_LAUNCH(k_gn_params, pgrid, dim3((unsigned)(waves * kWave)), 0, s, d, splits, dgamma, dbeta,
+              ldg);
   return hipGetLastError();
 }
 

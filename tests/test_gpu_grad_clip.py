@@ -12,7 +12,8 @@ from tests import operators_oracle as O
 pytestmark = pytest.mark.gpu
 
 DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
-# tensor sizes around a tile (2048 elements), a 16-byte vector, a word, and 1; many tiny ones; a large one
+# tensor sizes around a tile (2048 elements), a 16-byte vector, a word, and 1; many tiny
+# ones; a large one
 SIZES = {"one": [1], "small": [5, 64, 1, 3], "tile": [2047, 2048, 2049, 4096, 31, 7],
          "tiny": [1 + (i * 37) % 100 for i in range(300)], "large": [300_001, 70_000, 129]}
 SENTINEL = 7.25

@@ -304,7 +304,8 @@ def test_another_stream_and_graph_replays(shape):
 
 
 @pytest.mark.parametrize("dtype", list(DT))
-@pytest.mark.parametrize("shape", [(2, 2, 49, 64, 8), (1, 2, 3136, 64, 8), (1, 1, 65, 30, 5)], ids=str)
+@pytest.mark.parametrize("shape", [(2, 2, 49, 64, 8), (1, 2, 3136, 64, 8), (1, 1, 65, 30, 5)],
+                         ids=str)
 def test_features_at_odd_addresses(shape, dtype):
     """Features that start one element past an alignment boundary, as slices of larger
     buffers do: aligned ones may be read another way, so the results agree to rounding."""

@@ -63,7 +63,8 @@ def test_null_handles_are_rejected():
 @pytest.mark.parametrize("bad", [
     dict(K=0), dict(K=4097), dict(N=0), dict(P=0), dict(C=0), dict(C=65540), dict(G=0), dict(G=3),
     dict(dtype=-1), dict(dtype=3), dict(act=-1), dict(act=3), dict(eps=0.0), dict(eps=-1.0),
-    dict(eps=float("inf")), dict(eps=float("nan")), dict(P=1 << 40), dict(N=1 << 62)])
+    dict(eps=float("inf")), dict(eps=float("nan")), dict(P=1 << 40), dict(N=1 << 62),
+    dict(K=4096, C=65536, N=1, P=1)])
 def test_group_norm_shapes_are_checked(bad):
     from paper_2008_05823_amd import saef as S
     a = dict(dict(K=2, N=3, P=5, C=8, G=2, dtype=0, act=0, eps=1e-5), **bad)
