@@ -1527,9 +1527,9 @@ int saef_group_norm_create(int32_t K, int64_t N, int64_t P, int32_t C, int32_t G
   const saef::GroupNormHeld bwd = hold_group_norm(d, dtype, true);
   // a launch has at most 2^32 - 1 threads
   const double items = (double)K * (double)N;
-  if (items * d.slabs * d.splits * saef::kBlock >= 4294967296.0 ||
-      (double)K * ((C + saef::kWave - 1) / saef::kWave) * saef::kParamWaves * saef::kWave >=
-          4294967296.0 ||
+  const double params = (double)K * ((C + saef::kWave - 1) / saef::kWave);
+  if ((items * d.slabs * d.splits + params) * saef::kBlock >= 4294967296.0 ||
+      params * saef::kParamWaves * saef::kWave >= 4294967296.0 ||
       items * fwd.slabs * fwd.threads >= 4294967296.0 ||
       items * bwd.slabs * bwd.threads >= 4294967296.0)
     return SAEF_EINVAL;

@@ -472,6 +472,41 @@ __global__ __launch_bounds__(kBlock) void k_gn_bwd_sums(GroupNormDev d,
   }, [&](int i, double2 s) { out[i] = s; });
 }
 
+// dgamma and dbeta of 64 channels of a worker: the channel sums over its samples
+// and their pixel ranges, which are kept in fp32 (with a pixel or few a sample they are
+// as large as the features) and added up in binary64.  The workgroup's waves take
+// the rows in turn; block < K ceil(C / 64).
+__device__ __forceinline__ void param_sums(const GroupNormDev& d, int splits, unsigned block,
+                                           float* __restrict__ dgamma,
+                                           float* __restrict__ dbeta, int64_t ldg) {
+  double2* table = reinterpret_cast<double2*>(dyn_lds);  // [waves 64]
+  const unsigned per = (unsigned)((d.C + kWave - 1) / kWave);
+  const int k = (int)(block / per), waves = (int)blockDim.x / kWave;
+  const int c = (int)(block % per) * kWave + lane_id();
+  const int w = wave_id();
+  const int64_t rows = d.N * splits;
+  double2 s = make_double2(0.0, 0.0);
+  if (c < d.C) {
+    const float2* p = reinterpret_cast<const float2*>(d.part) + k * rows * d.C + c;
+#pragma unroll 4
+    for (int64_t i = w; i < rows; i += waves) {
+      const float2 v = p[i * d.C];
+      s.x += (double)v.x;
+      s.y += (double)v.y;
+    }
+  }
+  table[threadIdx.x] = s;
+  __syncthreads();
+  if (w != 0 || c >= d.C) return;
+  for (int i = 1; i < waves; ++i) {
+    s.x += table[i * kWave + lane_id()].x;
+    s.y += table[i * kWave + lane_id()].y;
+  }
+  dgamma[k * ldg + c] = (float)s.x;
+  dbeta[k * ldg + c] = (float)s.y;
+}
+
+// The first `params` workgroups take dgamma and dbeta along: a launch less.
 template <int kType, int kN, int kAct>
 __global__ __launch_bounds__(kBlock) void k_gn_bwd_apply(GroupNormDev d,
                                                          const void* __restrict__ dy,
@@ -481,9 +516,16 @@ __global__ __launch_bounds__(kBlock) void k_gn_bwd_apply(GroupNormDev d,
                                                          int64_t ld,
                                                          const float* __restrict__ mean,
                                                          const float* __restrict__ rstd,
-                                                         void* __restrict__ dx) {
+                                                         void* __restrict__ dx,
+                                                         float* __restrict__ dgamma,
+                                                         float* __restrict__ dbeta,
+                                                         int64_t ldg, unsigned params) {
   typedef typename Elem<kType>::T T;
-  const Part<kN> w(d, d.backwards ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+  if (blockIdx.x < params) {
+    param_sums(d, d.splits, blockIdx.x, dgamma, dbeta, ldg);
+    return;
+  }
+  const Part<kN> w(d, d.backwards ? gridDim.x - 1 - blockIdx.x : blockIdx.x - params);
   Stream<kType, kN, 2, true> in(w, x, dy);
   float2* st = reinterpret_cast<float2*>(dyn_lds);
   const int g0 = w.group0(d);
@@ -671,7 +713,8 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_fwd_held(GroupNormDev d,
   }
 }
 
-// dz is formed once and kept in fp32 beside x.  Grid: K N slabs workgroups.
+// dz is formed once and kept in fp32 beside x.  With one sample a worker its channel
+// sums are dgamma and dbeta.  Grid: K N slabs workgroups.
 template <int kType, int kAct, int kR, bool kOne>
 __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d,
                                                               const void* __restrict__ dy,
@@ -681,7 +724,10 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d,
                                                               int64_t ld,
                                                               const float* __restrict__ mean,
                                                               const float* __restrict__ rstd,
-                                                              void* __restrict__ dx) {
+                                                              void* __restrict__ dx,
+                                                              float* __restrict__ dgamma,
+                                                              float* __restrict__ dbeta,
+                                                              int64_t ldg) {
   constexpr int kN = Elem<kType>::kVec;
   constexpr int kA = kOne ? 1 : kN;
   const Held<kType, kR> w(d);
@@ -749,7 +795,8 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d,
     const float r = e == t ? r1 : rstd[g0 + c / d.Cg];
     const float ga = e == t ? ga1 : gamma[w.k * ld + w.c0 + c];
     if (e < cw) s *= (double)r;
-    part[2 * c + (e >= cw)] = (float)s;
+    if (d.N > 1) part[2 * c + (e >= cw)] = (float)s;
+    else (e < cw ? dgamma : dbeta)[w.k * ldg + w.c0 + c] = (float)s;
     ca[2 * c + (e >= cw)] = s * (double)ga;
   }
   __syncthreads();
@@ -781,39 +828,12 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d,
   }
 }
 
-// dgamma and dbeta: the channel sums over a worker's samples and pixel ranges, which
-// are kept in fp32 (with a pixel or few a sample they are as large as the features) and
-// added up in binary64.
-// Grid: K ceil(C / 64) workgroups of up to kParamWaves waves, which take the rows in turn.
-__global__ __launch_bounds__(kParamWaves* kWave) void k_gn_params(GroupNormDev d, int splits,
+// Grid: K ceil(C / 64) workgroups of up to kParamWaves waves.
+__global__ __launch_bounds__(kParamWaves* kWave) void k_gn_params(GroupNormDev d,
                                                                   float* __restrict__ dgamma,
                                                                   float* __restrict__ dbeta,
                                                                   int64_t ldg) {
-  __shared__ double2 s_p[kParamWaves][kWave];
-  const unsigned per = (unsigned)((d.C + kWave - 1) / kWave);
-  const int k = (int)(blockIdx.x / per), waves = (int)blockDim.x / kWave;
-  const int c = (int)(blockIdx.x % per) * kWave + lane_id();
-  const int w = wave_id();
-  const int64_t rows = d.N * splits;
-  double2 s = make_double2(0.0, 0.0);
-  if (c < d.C) {
-    const float2* p = reinterpret_cast<const float2*>(d.part) + k * rows * d.C + c;
-#pragma unroll 4
-    for (int64_t i = w; i < rows; i += waves) {
-      const float2 v = p[i * d.C];
-      s.x += (double)v.x;
-      s.y += (double)v.y;
-    }
-  }
-  s_p[w][lane_id()] = s;
-  __syncthreads();
-  if (w != 0 || c >= d.C) return;
-  for (int i = 1; i < waves; ++i) {
-    s.x += s_p[i][lane_id()].x;
-    s.y += s_p[i][lane_id()].y;
-  }
-  dgamma[k * ldg + c] = (float)s.x;
-  dbeta[k * ldg + c] = (float)s.y;
+  param_sums(d, 1, blockIdx.x, dgamma, dbeta, ldg);
 }
 
 // Calls f with the element type, the vector width and the activation as
@@ -924,43 +944,41 @@ hipError_t launch_group_norm_backward(const GroupNormDev& d, const GroupNormHeld
                                       const float* rstd, void* dx, float* dgamma, float* dbeta,
                                       int64_t ldg, hipStream_t s) {
   const LaunchEvents ev;
-  hipError_t err;
-  int splits = d.splits;
+  const unsigned params = (unsigned)d.K * (unsigned)((d.C + kWave - 1) / kWave);
   if (held.threads > 0 && aligned16(x, dy, dx)) {
     GroupNormDev h = d;
     h.slab = held.slab;
     h.slabs = held.slabs;
-    splits = 1;
     const bool one = d.Cg % (16 / dtype_bytes(dtype)) == 0;
     const size_t lds = group_norm_held_lds(d, held, dtype, true);
     const dim3 grid((unsigned)(d.K * d.N * h.slabs)), block((unsigned)held.threads);
-    err = dispatch_held(dtype, act, held.vectors, one, [&](auto type, auto a, auto r, auto o) {
+    const hipError_t err =
+        dispatch_held(dtype, act, held.vectors, one, [&](auto type, auto a, auto r, auto o) {
       constexpr int T = decltype(type)::value, A = decltype(a)::value, R = decltype(r)::value;
       constexpr bool O = decltype(o)::value;
       if constexpr (R <= 8)  // (16 do not fit the registers and are never chosen)
         SAEF_LAUNCH((k_gn_bwd_held<T, A, R, O>), grid, block, lds, s, h, dy, x, gamma, beta, ld,
-                    mean, rstd, dx);
+                    mean, rstd, dx, dgamma, dbeta, ldg);
     });
-  } else {
-    const dim3 grid((unsigned)(d.K * d.N * d.slabs * d.splits)), block(kBlock);
-    const size_t lds = ((size_t)places(d) * d.vec + 1) * sizeof(float2) +
-                       (size_t)d.slab * sizeof(double2);
-    const size_t means = ((size_t)d.slab / d.Cg + 2) * sizeof(float2);
-    err = dispatch(dtype, d.vec, act, [&](auto type, auto n, auto a) {
-      constexpr int T = decltype(type)::value, V = decltype(n)::value, A = decltype(a)::value;
-      SAEF_LAUNCH((k_gn_bwd_sums<T, V, A>), grid, block, lds, s, d, x, dy, gamma, beta, ld, mean,
-                  rstd);
-      SAEF_LAUNCH((k_gn_bwd_apply<T, V, A>), grid, block, means, s, d, dy, x, gamma, beta, ld,
-                  mean, rstd, dx);
-    });
+    if (err != hipSuccess || d.N == 1) return err;
+    // four rows a wave, on their way together
+    const int waves = (int)std::min<int64_t>(kParamWaves, (d.N + 3) / 4);
+    SAEF_LAUNCH(k_gn_params, dim3(params), dim3((unsigned)(waves * kWave)),
+                (size_t)(waves * kWave) * sizeof(double2), s, d, dgamma, dbeta, ldg);
+    return hipGetLastError();
   }
-  if (err != hipSuccess) return err;
-  const dim3 pgrid((unsigned)d.K * (unsigned)((d.C + kWave - 1) / kWave));
-  // four rows a wave, on their way together
-  const int waves = (int)std::min<int64_t>(kParamWaves, (d.N * splits + 3) / 4);
-  SAEF_LAUNCH(k_gn_params, pgrid, dim3((unsigned)(waves * kWave)), 0, s, d, splits, dgamma, dbeta,
-              ldg);
-  return hipGetLastError();
+  const unsigned parts = (unsigned)(d.K * d.N * d.slabs * d.splits);
+  const size_t lds = ((size_t)places(d) * d.vec + 1) * sizeof(float2) +
+                     (size_t)d.slab * sizeof(double2);
+  const size_t apply_lds = std::max(((size_t)d.slab / d.Cg + 2) * sizeof(float2),
+                                    (size_t)kBlock * sizeof(double2));
+  return dispatch(dtype, d.vec, act, [&](auto type, auto n, auto a) {
+    constexpr int T = decltype(type)::value, V = decltype(n)::value, A = decltype(a)::value;
+    SAEF_LAUNCH((k_gn_bwd_sums<T, V, A>), dim3(parts), dim3(kBlock), lds, s, d, x, dy, gamma, beta,
+                ld, mean, rstd);
+    SAEF_LAUNCH((k_gn_bwd_apply<T, V, A>), dim3(params + parts), dim3(kBlock), apply_lds, s, d, dy,
+                x, gamma, beta, ld, mean, rstd, dx, dgamma, dbeta, ldg, params);
+  });
 }
 
 }  // namespace saef
