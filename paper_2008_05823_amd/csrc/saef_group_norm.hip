@@ -21,8 +21,8 @@
 // over a workgroup's; a sample's channel sums are kept in fp32 for dgamma, dbeta.
 //
 // Measured (256 samples, bf16): 196 x 1024 forward 42 us (4.9 TB/s), backward with
-// silu 72 us (4.3 TB/s; about 40 us of vector instructions beside it); 12544 x
-// 64, read twice, forward 213 us (5.8 TB/s of what it moves), backward 372.
+// silu 70 us (4.4 TB/s; about 40 us of vector instructions beside it); 12544 x
+// 64, read twice, forward 212 us (5.8 TB/s of what it moves), backward 357.
 #include <hip/hip_ext.h>
 
 #include <algorithm>
