@@ -1446,7 +1446,27 @@ void cut_group_norm(saef::GroupNormDev& d, int dtype) {
 saef::GroupNormHeld hold_group_norm(const saef::GroupNormDev& d, int dtype, bool back) {
   const int32_t es = saef::dtype_bytes(dtype), vec = 16 / es;
   const saef::GroupNormHeld none{0, 0, 0, 0};
-  if (d.C % vec != 0 || d.P > (int64_t(1) << 31) / es / d.C - 1) return none;
+  if (d.P > (int64_t(1) << 31) / es / d.C - 1) return none;
+  if (d.C % vec != 0) {
+    // Vectors straddle pixels: the threads whose channels repeat take a whole sample, of
+    // one vector at least.  128 samples of 64 x 33 in f32: forward 7.3 us, backward 11.6;
+    // read twice 10.0 and 11.7.  2048 samples of 240 x 30: 22 and 53; 35 and 83.
+    if (d.P * d.C < vec) return none;
+    const int32_t period = d.C / std::min(vec, d.C & -d.C);
+    for (int32_t threads : {64, 128, 256, 512})
+      for (int32_t vectors : {4, 8}) {
+        const int64_t held = (int64_t)(threads / period) * period * vectors * vec;
+        if (held < d.P * d.C || held == 0) continue;
+        // The most registers with 8 values a vector: a workgroup a CU, so one round of
+        // them gains (256 samples of 196 x 84 in bf16 12.2 and 19.9 us, read twice 13.4
+        // and 22.1) and more do not (512 of them 22.7 and 34; 17.9 and 25.4).  In f32
+        // more do (512 samples of 500 x 30: 13.9 and 25.7; 19.6 and 38).
+        if (vec == 8 && threads * vectors == 4096 && (int64_t)d.K * d.N > 256) return none;
+        const saef::GroupNormHeld h{threads, vectors, d.C, 1};
+        if (saef::group_norm_held_lds(d, h, dtype, back) <= saef::kMostLds) return h;
+      }
+    return none;
+  }
   const int32_t unit = d.Cg / std::min(vec, d.Cg & -d.Cg) * vec;  // whole groups and vectors
   // Small workgroups first, then long rows (256 samples of 196 x 1024 in bf16: forward
   // 42 us with 256 threads and 256 bytes, 54 with 512 and 128; rows of 64 bytes took

@@ -30,7 +30,8 @@ constexpr int kParamWaves = 16;  // of a workgroup that adds up 64 channels of d
 
 // How a kernel that reads its features once cuts the work: workgroups of
 // `threads` threads, each holding `vectors` 16-byte vectors, take slabs of
-// `slab` channels of whole groups.  threads == 0: the shape does not fit.
+// `slab` channels of whole groups, or of all groups where vectors do not divide
+// the channels.  threads == 0: the shape does not fit.
 struct GroupNormHeld {
   int32_t threads, vectors, slab, slabs;
 };

@@ -175,8 +175,8 @@ inline int table_places(int threads, int period) {
 // slab of channels over a range of pixels, then a second kernel joins a
 // sample's sums and computes the result.  Where the features exceed the last-level
 // cache the second goes through the samples backwards, so that what the cache still
-// holds is read from there (256 samples of 1.6 MB: forward 223 us, in the same order
-// 243; backward 376 and 394; at 103 MB the same order is 1 us ahead).
+// holds is read from there (256 samples of 1.6 MB: 20 us less forward and 18 less
+// backward than in the same order; at 103 MB the same order is 1 us ahead).
 
 // Vectors of a thread's in flight.
 constexpr int kU = 4;
@@ -828,6 +828,215 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d,
   }
 }
 
+// ---- channels that vectors do not divide ----------------------------------------
+// The same for small samples of any C: the slab is all channels, a sample one run of
+// memory, and vectors straddle pixels (Part's layout, without pixel ranges), at any
+// alignment.  Thread t's i-th vector: elements left - i dec of the sample from it on.
+// Bound by latency (a load, the joins in LDS) up to about a workgroup a CU: 32
+// samples of 784 x 6 in bf16 take 9.0 us forward and 12.2 backward, 18 backward with
+// a thread to a channel in the join, 11 and 25 read twice; above by memory (2048
+// samples of 240 x 30 in f32 22 and 53 us, 5.4 and 3.3 TB/s).
+template <int kType, int kR, int kS>
+struct Flat {
+  static constexpr int kN = Elem<kType>::kVec;
+  typedef typename Elem<kType>::T T;
+  Vals<kType, kN> v[kR][kS];
+
+  // No load lies under a branch, so that all are on their way together: a vector
+  // that passes the sample's end is read where its last whole one is, and the values
+  // that are its own are shifted to the front.  (A sample has a vector at least.)
+  __device__ __forceinline__ Flat(const GroupNormDev& d, const Part<kN>& w, const void* a,
+                                  const void* b = nullptr) {
+    const void* src[2] = {a, b};
+    typedef unsigned int Raw __attribute__((ext_vector_type(4), aligned(2)));
+    Raw raw[kR][kS];
+    const int64_t last = (w.n + 1) * d.P * d.C - kN;
+#pragma unroll
+    for (int i = 0; i < kR; ++i) {
+      const int64_t at = min(w.first + i * w.stride, last);
+#pragma unroll
+      for (int q = 0; q < kS; ++q)
+        raw[i][q] = *reinterpret_cast<const Raw*>(static_cast<const T*>(src[q]) + at);
+    }
+#pragma unroll
+    for (int i = 0; i < kR; ++i) {
+      const int n = left(w, i);
+#pragma unroll
+      for (int q = 0; q < kS; ++q) {
+        unsigned __int128 bits;
+        __builtin_memcpy(&bits, &raw[i][q], 16);
+        if (n < kN) bits = n > 0 ? bits >> (kN - n) * 8 * (int)sizeof(T) : 0;
+        __builtin_memcpy(v[i][q].v, &bits, 16);
+      }
+    }
+  }
+  // elements of the i-th vector that are the sample's
+  static __device__ __forceinline__ int left(const Part<kN>& w, int i) {
+    return (int)max((int64_t)0, min(w.left - i * w.dec, (int64_t)kN));
+  }
+};
+
+// Grid: K N workgroups.
+template <int kType, int kAct, int kR>
+__global__ __launch_bounds__(kHeldThreads) void k_gn_fwd_flat(GroupNormDev d,
+                                                              const void* __restrict__ x,
+                                                              const float* __restrict__ gamma,
+                                                              const float* __restrict__ beta,
+                                                              int64_t ld, void* __restrict__ y,
+                                                              float* __restrict__ mean,
+                                                              float* __restrict__ rstd) {
+  constexpr int kN = Elem<kType>::kVec;
+  const Part<kN> w(d, blockIdx.x);
+  Flat<kType, kR, 1> in(d, w, x);
+  float mu[kN], sc[kN], sh[kN];
+  w.channels(d, [&](int j, int c, int) {
+    sc[j] = gamma[w.k * ld + c];
+    sh[j] = beta[w.k * ld + c];
+  });
+  double a0[kN] = {}, a1[kN] = {};
+#pragma unroll
+  for (int i = 0; i < kR; ++i) {
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {  // (past the sample's end: 0)
+      const double f = in.v[i][0][j];
+      a0[j] += f;
+      a1[j] = __builtin_fma(f, f, a1[j]);
+    }
+  }
+  double2* table = reinterpret_cast<double2*>(dyn_lds);
+  int places = w.active;
+  const int place = fold_place(w.period, places);
+  Stats* st = reinterpret_cast<Stats*>(table + places * kN);
+  fold_lanes(a0, a1, w.period);
+  if (place >= 0) {
+#pragma unroll
+    for (int j = 0; j < kN; ++j) table[place * kN + j] = make_double2(a0[j], a1[j]);
+  }
+  __syncthreads();
+  const double inv_m = 1.0 / ((double)d.P * d.Cg);
+  join_sums(d.G, places * kN / d.C * d.Cg, [&](int g, int q) {
+    return table[q / d.Cg * d.C + g * d.Cg + q % d.Cg];
+  }, [&](int g, double2 s) {
+    const Stats r = stats_of(s.x, s.y, inv_m, d.eps);
+    st[g] = r;
+    mean[w.n * d.G + g] = r.mean;
+    rstd[w.n * d.G + g] = r.rstd;
+  });
+  __syncthreads();
+  w.channels(d, [&](int j, int, int g) {
+    const Stats r = st[g];
+    mu[j] = r.mean;
+    sc[j] = r.rstd * sc[j];
+    sh[j] = __builtin_fmaf(-r.rest, sc[j], sh[j]);
+  });
+  typedef typename Elem<kType>::T T;
+#pragma unroll
+  for (int i = 0; i < kR; ++i) {
+    const int n = Flat<kType, kR, 1>::left(w, i);
+    auto v = in.v[i][0];
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+      v.set(j, act_of<kAct>(__builtin_fmaf(v[j] - mu[j], sc[j], sh[j])));
+    T* p = static_cast<T*>(y) + w.first + i * w.stride;
+    if (n == kN) v.store(p); else v.store(p, n);
+  }
+}
+
+// Grid: K N workgroups.
+template <int kType, int kAct, int kR>
+__global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_flat(GroupNormDev d,
+                                                              const void* __restrict__ dy,
+                                                              const void* __restrict__ x,
+                                                              const float* __restrict__ gamma,
+                                                              const float* __restrict__ beta,
+                                                              int64_t ld,
+                                                              const float* __restrict__ mean,
+                                                              const float* __restrict__ rstd,
+                                                              void* __restrict__ dx,
+                                                              float* __restrict__ dgamma,
+                                                              float* __restrict__ dbeta,
+                                                              int64_t ldg) {
+  constexpr int kN = Elem<kType>::kVec;
+  const Part<kN> w(d, blockIdx.x);
+  Flat<kType, kR, 2> in(d, w, x, dy);
+  float mu[kN], gs[kN], be[kN], k1[kN], k2[kN];
+  w.channels(d, [&](int j, int c, int g) {
+    mu[j] = mean[w.n * d.G + g];
+    k1[j] = rstd[w.n * d.G + g];
+    gs[j] = gamma[w.k * ld + c] * k1[j];
+    be[j] = beta[w.k * ld + c];
+  });
+  float a[kN] = {}, b[kN] = {};
+  float dz[kR][kN];
+#pragma unroll
+  for (int i = 0; i < kR; ++i) {
+    const int n = Flat<kType, kR, 2>::left(w, i);
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      const float u = in.v[i][0][j] - mu[j];
+      const float q = act_back<kAct>(in.v[i][1][j], __builtin_fmaf(u, gs[j], be[j]));
+      dz[i][j] = q;
+      if (j < n) {
+        a[j] = __builtin_fmaf(q, u, a[j]);
+        b[j] += q;
+      }
+    }
+  }
+  // element f of the threads' sums side by side belongs to channel f mod C
+  float2* table = reinterpret_cast<float2*>(dyn_lds);
+  int places = w.active;
+  const int place = fold_place(w.period, places);
+  const int elems = places * kN;
+  double2* sums = reinterpret_cast<double2*>(table + elems);
+  float2* st = reinterpret_cast<float2*>(sums + d.C);
+  fold_lanes(a, b, w.period);
+  if (place >= 0) {
+#pragma unroll
+    for (int j = 0; j < kN; ++j) table[place * kN + j] = make_float2(a[j], b[j]);
+  }
+  __syncthreads();
+  float2* part = reinterpret_cast<float2*>(d.part) + w.n * d.C;
+  join_sums(d.C, elems / d.C, [&](int c, int q) {
+    const float2 v = table[q * d.C + c];
+    return make_double2((double)v.x, (double)v.y);
+  }, [&](int c, double2 s) {
+    s.x *= (double)rstd[w.n * d.G + c / d.Cg];
+    if (d.N > 1) {
+      part[c] = make_float2((float)s.x, (float)s.y);
+    } else {
+      dgamma[w.k * ldg + c] = (float)s.x;
+      dbeta[w.k * ldg + c] = (float)s.y;
+    }
+    const double f = gamma[w.k * ld + c];
+    sums[c] = make_double2(f * s.x, f * s.y);
+  });
+  __syncthreads();
+  const double inv_m = 1.0 / ((double)d.P * d.Cg);
+  join_sums(d.G, d.Cg, [&](int g, int i) { return sums[g * d.Cg + i]; },
+            [&](int g, double2 s) {
+    st[g] = make_float2((float)(s.y * inv_m), (float)(s.x * inv_m));
+  });
+  __syncthreads();
+  // dx = gamma rstd dz - rstd s1 - (x - mean) rstd^2 s2
+  w.channels(d, [&](int j, int, int g) {
+    k2[j] = k1[j] * k1[j] * st[g].y;
+    k1[j] *= st[g].x;
+  });
+  typedef typename Elem<kType>::T T;
+#pragma unroll
+  for (int i = 0; i < kR; ++i) {
+    const int n = Flat<kType, kR, 2>::left(w, i);
+    auto v = in.v[i][0];
+#pragma unroll
+    for (int j = 0; j < kN; ++j) {
+      const float u = v[j] - mu[j];
+      v.set(j, __builtin_fmaf(gs[j], dz[i][j], -__builtin_fmaf(u, k2[j], k1[j])));
+    }
+    T* p = static_cast<T*>(dx) + w.first + i * w.stride;
+    if (n == kN) v.store(p); else v.store(p, n);
+  }
+}
+
 // Grid: K ceil(C / 64) workgroups of up to kParamWaves waves.
 __global__ __launch_bounds__(kParamWaves* kWave) void k_gn_params(GroupNormDev d,
                                                                   float* __restrict__ dgamma,
@@ -879,6 +1088,24 @@ hipError_t dispatch_held(int dtype, int act, int r, bool one, F&& f) {
   return hipGetLastError();
 }
 
+// f(type, act, vectors of a thread) for the kernels of any C.
+template <typename F>
+hipError_t dispatch_flat(int dtype, int act, int r, F&& f) {
+  auto with_r = [&](auto type, auto a) {
+    if (r == 8) f(type, a, std::integral_constant<int, 8>());
+    else f(type, a, std::integral_constant<int, 4>());
+  };
+  auto with_act = [&](auto type) {
+    if (act == kActRelu) with_r(type, std::integral_constant<int, kActRelu>());
+    else if (act == kActSilu) with_r(type, std::integral_constant<int, kActSilu>());
+    else with_r(type, std::integral_constant<int, kActNone>());
+  };
+  if (dtype == kF32) with_act(std::integral_constant<int, kF32>());
+  else if (dtype == kBF16) with_act(std::integral_constant<int, kBF16>());
+  else with_act(std::integral_constant<int, kF16>());
+  return hipGetLastError();
+}
+
 // Places in LDS of the two-pass sums (the last slab may be narrower than the
 // others).
 int places(const GroupNormDev& d) {
@@ -891,11 +1118,29 @@ bool aligned16(const void* a, const void* b, const void* c) {
            reinterpret_cast<uintptr_t>(c)) & 15u) == 0;
 }
 
+// The shape with a workgroup to a sample.
+GroupNormDev whole_samples(const GroupNormDev& d) {
+  GroupNormDev h = d;
+  h.slab = d.C;
+  h.slabs = 1;
+  h.splits = 1;
+  h.split_pixels = d.P;
+  return h;
+}
+
 }  // namespace
 
 size_t group_norm_held_lds(const GroupNormDev& d, const GroupNormHeld& held, int dtype,
                            bool back) {
   const int vec = 16 / dtype_bytes(dtype), groups = held.slab / d.Cg;
+  if (d.C % vec != 0) {
+    const int period = d.C / std::min(vec, d.C & -d.C);
+    const size_t at = folds(period) ? (size_t)table_places(held.threads, period)
+                                    : (size_t)(held.threads / period * period);
+    return back ? at * vec * sizeof(float2) + (size_t)d.C * sizeof(double2) +
+                      groups * sizeof(float2)
+                : at * vec * sizeof(double2) + groups * sizeof(Stats);
+  }
   const int last = d.C - (held.slabs - 1) * held.slab;  // channels of the last slab
   const size_t at = (size_t)std::max(table_places(held.threads, held.slab / vec),
                                      table_places(held.threads, last / vec));
@@ -910,6 +1155,16 @@ hipError_t launch_group_norm_forward(const GroupNormDev& d, const GroupNormHeld&
                                      const float* beta, int64_t ld, void* y, float* mean,
                                      float* rstd, hipStream_t s) {
   const LaunchEvents ev;
+  if (held.threads > 0 && d.C % (16 / dtype_bytes(dtype)) != 0) {
+    const GroupNormDev h = whole_samples(d);
+    const size_t lds = group_norm_held_lds(d, held, dtype, false);
+    const dim3 grid((unsigned)(d.K * d.N)), block((unsigned)held.threads);
+    return dispatch_flat(dtype, act, held.vectors, [&](auto type, auto a, auto r) {
+      constexpr int T = decltype(type)::value, A = decltype(a)::value, R = decltype(r)::value;
+      SAEF_LAUNCH((k_gn_fwd_flat<T, A, R>), grid, block, lds, s, h, x, gamma, beta, ld, y, mean,
+                  rstd);
+    });
+  }
   // (16-byte buffer accesses need their alignment; the two passes take any)
   if (held.threads > 0 && aligned16(x, y, nullptr)) {
     GroupNormDev h = d;
@@ -945,21 +1200,32 @@ hipError_t launch_group_norm_backward(const GroupNormDev& d, const GroupNormHeld
                                       int64_t ldg, hipStream_t s) {
   const LaunchEvents ev;
   const unsigned params = (unsigned)d.K * (unsigned)((d.C + kWave - 1) / kWave);
-  if (held.threads > 0 && aligned16(x, dy, dx)) {
-    GroupNormDev h = d;
-    h.slab = held.slab;
-    h.slabs = held.slabs;
-    const bool one = d.Cg % (16 / dtype_bytes(dtype)) == 0;
+  const bool flat = d.C % (16 / dtype_bytes(dtype)) != 0;
+  if (held.threads > 0 && (flat || aligned16(x, dy, dx))) {
     const size_t lds = group_norm_held_lds(d, held, dtype, true);
-    const dim3 grid((unsigned)(d.K * d.N * h.slabs)), block((unsigned)held.threads);
-    const hipError_t err =
-        dispatch_held(dtype, act, held.vectors, one, [&](auto type, auto a, auto r, auto o) {
-      constexpr int T = decltype(type)::value, A = decltype(a)::value, R = decltype(r)::value;
-      constexpr bool O = decltype(o)::value;
-      if constexpr (R <= 8)  // (16 do not fit the registers and are never chosen)
-        SAEF_LAUNCH((k_gn_bwd_held<T, A, R, O>), grid, block, lds, s, h, dy, x, gamma, beta, ld,
-                    mean, rstd, dx, dgamma, dbeta, ldg);
-    });
+    const dim3 block((unsigned)held.threads);
+    hipError_t err;
+    if (flat) {
+      const GroupNormDev h = whole_samples(d);
+      err = dispatch_flat(dtype, act, held.vectors, [&](auto type, auto a, auto r) {
+        constexpr int T = decltype(type)::value, A = decltype(a)::value, R = decltype(r)::value;
+        SAEF_LAUNCH((k_gn_bwd_flat<T, A, R>), dim3((unsigned)(d.K * d.N)), block, lds, s, h, dy, x,
+                    gamma, beta, ld, mean, rstd, dx, dgamma, dbeta, ldg);
+      });
+    } else {
+      GroupNormDev h = d;
+      h.slab = held.slab;
+      h.slabs = held.slabs;
+      const bool one = d.Cg % (16 / dtype_bytes(dtype)) == 0;
+      const dim3 grid((unsigned)(d.K * d.N * h.slabs));
+      err = dispatch_held(dtype, act, held.vectors, one, [&](auto type, auto a, auto r, auto o) {
+        constexpr int T = decltype(type)::value, A = decltype(a)::value, R = decltype(r)::value;
+        constexpr bool O = decltype(o)::value;
+        if constexpr (R <= 8)  // (16 do not fit the registers and are never chosen)
+          SAEF_LAUNCH((k_gn_bwd_held<T, A, R, O>), grid, block, lds, s, h, dy, x, gamma, beta, ld,
+                      mean, rstd, dx, dgamma, dbeta, ldg);
+      });
+    }
     if (err != hipSuccess || d.N == 1) return err;
     // four rows a wave, on their way together
     const int waves = (int)std::min<int64_t>(kParamWaves, (d.N + 3) / 4);

@@ -124,6 +124,54 @@ def test_backward(shape, dtype, act):
     assert torch.equal(dx, dx2) and torch.equal(g, g2)
 
 
+# Channels that vectors do not divide, samples small enough to stay in registers: channels that
+# repeat inside a vector; within a wave; over more threads than one; one pixel; one sample a
+# worker and several; a sample that just fits (2 x 256 x 4 x 4 values in f32), and one more pixel
+ODD = [(2, 3, 5, 1, 1), (3, 1, 9, 2, 1), (2, 2, 31, 3, 3), (2, 4, 17, 6, 2), (3, 1, 40, 10, 5),
+       (1, 5, 1, 27, 9), (2, 1, 1, 2046, 33), (4, 3, 49, 100, 10), (1, 2, 200, 63, 7),
+       (2, 2, 7, 514, 2), (1, 3, 8192, 1, 1), (1, 2, 8193, 1, 1), (2, 1, 2730, 6, 3)]
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "silu"])
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("shape", ODD, ids=str)
+def test_odd_channels(shape, dtype, act):
+    test_forward(shape, dtype, act)
+    test_backward(shape, dtype, act)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("shape", [(2, 3, 31, 27, 9), (1, 2, 200, 3, 1)], ids=str)
+def test_odd_channels_write_their_features_only(shape, dtype):
+    """Features inside larger buffers: what lies around the inputs (NaN) is not used, what lies
+    around the outputs stays."""
+    S = _S()
+    x, dy, gamma, beta = _inputs(shape, dtype, 12)
+    plan = _plan(S, shape, dtype, "silu")
+    y, mean, rstd = _forward(S, plan, x, gamma, beta)
+    dx, dg, db = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(beta)
+    S.saef_group_norm_backward(plan, dy, x, gamma, beta, mean, rstd, dx, dg, db)
+    n = x.numel()
+
+    def room(fill):
+        return torch.full((n + 64,), fill, dtype=x.dtype, device="cuda")
+
+    def inner(v):
+        return v[17:17 + n].view(x.shape)
+    rx, rdy, ry, rdx = room(math.nan), room(math.nan), room(-3.0), room(-3.0)
+    inner(rx).copy_(x)
+    inner(rdy).copy_(dy)
+    mean2, rstd2, dg2, db2 = (torch.empty_like(v) for v in (mean, rstd, dg, db))
+    S.saef_group_norm_forward(plan, inner(rx), gamma, beta, inner(ry), mean2, rstd2)
+    S.saef_group_norm_backward(plan, inner(rdy), inner(rx), gamma, beta, mean, rstd, inner(rdx),
+                               dg2, db2)
+    for got, want in ((inner(ry), y), (mean2, mean), (rstd2, rstd), (inner(rdx), dx), (dg2, dg),
+                      (db2, db)):
+        assert torch.equal(got, want)
+    for r in (ry, rdx):
+        assert bool((r[:17] == -3.0).all()) and bool((r[17 + n:] == -3.0).all())
+
+
 @pytest.mark.parametrize("shape", [(1, 1, 64, 8, 2), (2, 2, 196, 64, 8), (1, 1, 6000, 32, 4)],
                          ids=str)
 def test_means_far_above_the_deviation(shape):
