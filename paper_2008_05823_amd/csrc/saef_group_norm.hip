@@ -114,11 +114,12 @@ extern __shared__ __align__(16) unsigned char dyn_lds[];
 
 // Joins pairs of sums: put(i, sum of at(i, 0), at(i, 1), ...) for i < count, of up
 // to `terms` terms each.  A power of two of lanes adds up one of them, few enough
-// that all of them are under way at once.  All threads of the workgroup call it.
+// that `most` of them (count, or more) are under way at once: the order of a sum
+// depends on `terms` and `most` alone.  All threads of the workgroup call it.
 template <typename At, typename Put>
-__device__ __forceinline__ void join_sums(int count, int terms, At at, Put put) {
+__device__ __forceinline__ void join_sums(int count, int most, int terms, At at, Put put) {
   int lanes = 1;
-  while (lanes < kWave && lanes < terms && 2 * lanes * count <= (int)blockDim.x) lanes *= 2;
+  while (lanes < kWave && lanes < terms && 2 * lanes * most <= (int)blockDim.x) lanes *= 2;
   const int l = (int)threadIdx.x & (lanes - 1), per = (int)blockDim.x / lanes;
   for (int base = 0; base < count; base += per) {
     const int i = base + (int)threadIdx.x / lanes;
@@ -137,6 +138,10 @@ __device__ __forceinline__ void join_sums(int count, int terms, At at, Put put) 
     }
     if (i < count && l == 0) put(i, s);
   }
+}
+template <typename At, typename Put>
+__device__ __forceinline__ void join_sums(int count, int terms, At at, Put put) {
+  join_sums(count, count, terms, at, put);
 }
 
 // Before a workgroup's threads lay their sums side by side in LDS: where the
@@ -319,7 +324,10 @@ __device__ __forceinline__ void join_groups(const GroupNormDev& d, const Part<kN
     join_sums(w.groups(d), d.splits, [&](int i, int q) { return pieces[(int64_t)q * Q + i]; }, put);
     return;
   }
-  join_sums(w.groups(d), d.splits * span, [&](int i, int q) {
+  // Every slab of a group joins the same pieces; in one order, that of a slab that meets
+  // as many groups as one may, they come to the same statistics.
+  const int most = (d.slab + d.Cg - 2) / d.Cg + 1;
+  join_sums(w.groups(d), most, d.splits * span, [&](int i, int q) {
     const int g = w.group0(d) + i, b = g * d.Cg / d.slab + q % span;
     if (b > (g * d.Cg + d.Cg - 1) / d.slab) return make_double2(0.0, 0.0);
     return pieces[(int64_t)(q / span) * Q + g + b];
@@ -383,8 +391,8 @@ __global__ __launch_bounds__(kBlock) void k_gn_fwd_apply(GroupNormDev d,
   join_groups(d, w, [&](int i, double2 s) {
     const Stats r = stats_of(s.x, s.y, inv_m, d.eps);
     st[i] = r;
-    // (a group in several slabs: all write the same)
-    if (w.s == 0) {
+    // (a group in several slabs: the one of its first channel)
+    if (w.s == 0 && (g0 + i) * d.Cg >= w.c0) {
       mean[w.n * d.G + g0 + i] = r.mean;
       rstd[w.n * d.G + g0 + i] = r.rstd;
     }
