@@ -15,6 +15,14 @@ pytestmark = pytest.mark.gpu
 SPANNING = [(1, 2, 100, 441, 7), (1, 1, 60, 1030, 5), (2, 1, 400, 520, 8), (1, 1, 400, 1024, 1)]
 
 
+@pytest.mark.parametrize("act", ["none", "relu", "silu"])
+@pytest.mark.parametrize("dtype", list(T.DT))
+@pytest.mark.parametrize("shape", SPANNING, ids=str)
+def test_groups_across_slabs(shape, dtype, act):
+    T.test_forward(shape, dtype, act)
+    T.test_backward(shape, dtype, act)
+
+
 @pytest.mark.parametrize("shape", [(1, 32, 3408, 273, 7)] + SPANNING, ids=str)
 def test_a_group_has_the_same_statistics_in_all_its_slabs(shape):
     """Channels with the same values, gamma and beta in one group get the same y and dx bit for
@@ -46,3 +54,8 @@ def test_a_group_has_the_same_statistics_in_all_its_slabs(shape):
     for _ in range(3):
         for a, b in zip(first, run()):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("shape", SPANNING, ids=str)
+def test_means_far_above_the_deviation(shape):
+    T.test_means_far_above_the_deviation(shape)
