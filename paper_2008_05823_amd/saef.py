@@ -366,11 +366,18 @@ class GroupNorm:
 
     def _features(self, t, what):
         """Address of K N P C features: a contiguous tensor whose last dimension is
-        C, or (K N, C, H, W) in torch's channels_last memory format."""
-        if t.dtype == self.dtype and t.is_cuda and t.numel() == self.numel and t.dim() > 0 \
-                and t.shape[-1] == self.C and t.is_contiguous():
+        C, or (K N, C, H, W) in torch's channels_last memory format.  A contiguous
+        (K N, C, H, C) may be channels first or last and is refused."""
+        shape = t.shape
+        either = len(shape) == 4 and shape[1] == self.C and shape[0] == self.K * self.N \
+            and self.C > 1
+        if t.dtype == self.dtype and t.is_cuda and t.numel() == self.numel and len(shape) > 0 \
+                and shape[-1] == self.C and not either and t.is_contiguous():
             return t.data_ptr()
         _sized(t, self.numel, what)  # else: the other layout, or why not
+        if either and shape[3] == self.C and t.is_contiguous():
+            raise ValueError(f"{what} of shape {tuple(shape)} may be channels first or last: pass "
+                             "it as (K, N, P, C), or channels first in the channels_last format")
         if t.dim() == 0 or t.shape[-1] != self.C or not t.is_contiguous():
             if t.dim() != 4 or t.shape[:2] != (self.K * self.N, self.C) \
                     or not t.is_contiguous(memory_format=torch.channels_last):
