@@ -286,6 +286,7 @@ class Grads:
     def handle(self):
         if self._h is None:
             raise ValueError("gradients destroyed")
+        self.layout.handle  # (raises if the layout was closed: its memory is gone)
         return self._h
 
     def destroy(self):
@@ -473,6 +474,7 @@ class TopK:
     def handle(self):
         if self._h is None:
             raise ValueError("plan destroyed")
+        self.layout.handle  # (raises if the layout was closed: its memory is gone)
         return self._h
 
     def destroy(self):
