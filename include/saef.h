@@ -247,6 +247,10 @@ int saef_group_norm_forward(const saef_group_norm* plan, const void* x, const fl
  * at dgamma + k ldg and dbeta + k ldg, e.g. in its gradient row; overwritten),
  * summed over its samples in a fixed order.  x, gamma, beta as in the forward
  * call, mean and rstd as it left them.  relu: the derivative at z <= 0 is 0.
+ * The gradient is that at these fp32 statistics.  The forward call also applies
+ * what rounding the mean to fp32 leaves, so the two values of (x - mean) rstd
+ * differ by up to 2^-24 |mean| rstd (6e-4 where the mean is 10^4 deviations), and
+ * so may the side of relu's kink for z that close to it.
  * The outputs must not overlap the inputs or one another; rows of dgamma and
  * dbeta may interleave. */
 int saef_group_norm_backward(const saef_group_norm* plan, const void* dy, const void* x,
