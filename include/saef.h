@@ -266,8 +266,9 @@ int saef_group_norm_backward(const saef_group_norm* plan, const void* dy, const 
  *   g_ki  <- fp32(c_k g_ki), rounded again to a 16-bit output
  * Squares are exact in binary64 and summed there, in a fixed order of the
  * library's own: norms are the same from run to run, and agree with the
- * exact ones to within an fp32 rounding and n 2^-53.  An infinite value makes
- * norm_k infinite and c_k 0; one that is no number makes norm_k and c_k none,
+ * exact ones to within an fp32 rounding and n 2^-53.  An infinite value, or a
+ * norm above the largest fp32 number, makes norm_k infinite and c_k 0 (0 times an
+ * infinite value is no number); one that is no number makes norm_k and c_k none,
  * and the worker's whole gradient with it, which the compression reports as
  * SAEF_ERANGE.
  *
@@ -276,7 +277,8 @@ int saef_group_norm_backward(const saef_group_norm* plan, const void* dy, const 
  * of worker k, of type dtype, aligned to an element: a row of the layout at
  * off[l], a tensor that automatic differentiation filled, or a piece of a
  * bucket.  No two may overlap; the memory must stay while the handle is
- * used.  The handle owns device scratch: 8 bytes per (tensor, worker), and up
+ * used.  The addresses are those at creation: gradients that are allocated anew
+ * need a new handle.  The handle owns device scratch: 8 bytes per (tensor, worker), and up
  * to 16 per (tile, worker).  Calls that use one saef_grads must not run
  * concurrently.  Synchronous; the layout must outlive the handle. */
 typedef struct saef_grads saef_grads;

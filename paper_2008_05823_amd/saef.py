@@ -250,7 +250,10 @@ class Grads:
     """Where K workers' gradients lie (see saef_grads_create).  src: the rows of
     a (K, d_pad) tensor, or one sequence per worker of its L tensors in layout
     order (any shapes of n[l] elements, contiguous); fp32, bf16 or fp16
-    throughout.  The tensors are kept alive."""
+    throughout.  The tensors are kept alive, and it is these that every call reads or
+    scales: gradients that lie elsewhere afterwards, as after
+    ``zero_grad(set_to_none=True)`` (the default), need a Grads of their own; with
+    ``set_to_none=False`` they stay where they are."""
 
     def __init__(self, layout: "Layout", src):
         if isinstance(src, torch.Tensor):
