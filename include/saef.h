@@ -228,10 +228,13 @@ int saef_materialize(const saef_layout* layout, int32_t K, int32_t mode, const f
  * for parameters in the rows of xh (C contiguous values, ld >= C).
  * Statistics are formed in binary64, the rest in fp32; y is rounded once, to
  * dtype.  mean, rstd: (K, N, G), for the backward pass.
- * A group norm is planned for one shape; the plan owns at most 24 bytes of
- * device scratch per channel, sample and pixel range (one range per 2048 to 8192
- * loads of a sample).  Calls that use one plan must not run concurrently.
- *  K <= 4096, C <= 65536, G divides C, eps > 0. */
+ * A group norm is planned for one shape; the plan owns at most 8 C +
+ * 16 (G + C / 128) bytes of device scratch per sample and pixel range (one range,
+ * or ranges of at least 2048 loads of a slab; slabs of 128 channels or more make
+ * up the C).  Calls that use one plan must not run concurrently.
+ *  K <= 4096, C <= 65536, K N P C <= 2^40, G divides C, eps > 0; shapes whose
+ *  launches would take 2^32 threads or more (up to 512 per sample, slab and
+ *  range) are refused. */
 typedef struct saef_group_norm saef_group_norm;
 
 int saef_group_norm_create(int32_t K, int64_t N, int64_t P, int32_t C, int32_t G, int32_t dtype,
