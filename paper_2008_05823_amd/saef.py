@@ -289,7 +289,8 @@ class Grads:
     def handle(self):
         if self._h is None:
             raise ValueError("gradients destroyed")
-        self.layout.handle  # (raises if the layout was closed: its memory is gone)
+        if self.layout._h is None:
+            raise ValueError("layout destroyed")
         return self._h
 
     def destroy(self):
@@ -477,7 +478,8 @@ class TopK:
     def handle(self):
         if self._h is None:
             raise ValueError("plan destroyed")
-        self.layout.handle  # (raises if the layout was closed: its memory is gone)
+        if self.layout._h is None:
+            raise ValueError("layout destroyed")
         return self._h
 
     def destroy(self):
