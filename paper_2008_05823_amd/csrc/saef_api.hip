@@ -1431,8 +1431,9 @@ void cut_group_norm(saef::GroupNormDev& d, int dtype) {
   d.slabs = (d.C + d.slab - 1) / d.slab;
   // About 2 workgroups for each of the 256 CUs (more make the second pass join more
   // sums: 50 MB forward 20.6 us, 24 with 4), of at least 8 vectors a thread, and at most
-  // 32 (the backward sums add a thread's values in fp32, and long workgroups leave CUs
-  // idle at the end: 256 samples of 1.6 MB forward 218 us, 226 with 64).
+  // 32, or 64 where half of the threads have no whole pixels (the backward sums add a
+  // thread's values in fp32, and long workgroups leave CUs idle at the end: 256 samples of
+  // 1.6 MB forward 218 us, 226 with twice as many).
   const int64_t wgs = 512;
   const int64_t items = (int64_t)d.K * d.N * d.slabs, round = (int64_t)saef::kBlock * d.vec;
   const int64_t most = d.P * d.slab / (round * 8), least = d.P * d.slab / (round * 32) + 1;

@@ -634,7 +634,8 @@ __device__ __forceinline__ u32x4 raw_of(const Vals<kType, Elem<kType>::kVec>& v)
 
 // Makes the compiler unpack the vectors again where they are used next, instead of
 // keeping their values in twice the registers meanwhile (16-bit features, 8
-// vectors a thread, forward: 88 registers, 118 otherwise).
+// vectors a thread, forward: 96 registers, 116 otherwise; 99 and 160 where a vector
+// meets several groups).
 template <int kR>
 __device__ __forceinline__ void packed(u32x4 (&raw)[kR]) {
 #pragma unroll
