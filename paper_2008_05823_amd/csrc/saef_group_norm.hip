@@ -539,11 +539,11 @@ __global__ __launch_bounds__(kBlock) void k_gn_bwd_apply(GroupNormDev d,
   Stream<kType, kN, 2, true> in(w, x, dy);
   float2* st = reinterpret_cast<float2*>(dyn_lds);
   const int g0 = w.group0(d);
-  float mu[kN], gs[kN], be[kN], k1[kN], k2[kN];
+  float mu[kN], rs[kN], gs[kN], be[kN], k1[kN], k2[kN];
   w.channels(d, [&](int j, int c, int g) {
     mu[j] = mean[w.n * d.G + g];
-    k1[j] = rstd[w.n * d.G + g];
-    gs[j] = gamma[w.k * ld + c] * k1[j];
+    rs[j] = rstd[w.n * d.G + g];
+    gs[j] = gamma[w.k * ld + c] * rs[j];
     be[j] = beta[w.k * ld + c];
   });
   const double inv_m = 1.0 / ((double)d.P * d.Cg);
@@ -552,17 +552,17 @@ __global__ __launch_bounds__(kBlock) void k_gn_bwd_apply(GroupNormDev d,
   });
   __syncthreads();
   if (w.left <= 0) return;
-  // dx = gamma rstd dz - rstd s1 - (x - mean) rstd^2 s2
+  // dx = gamma rstd dz - rstd s1 - ((x - mean) rstd) (rstd s2)
   w.channels(d, [&](int j, int, int g) {
-    k2[j] = k1[j] * k1[j] * st[g - g0].y;
-    k1[j] *= st[g - g0].x;
+    k1[j] = rs[j] * st[g - g0].x;
+    k2[j] = rs[j] * st[g - g0].y;
   });
   in.each([&](Vals<kType, kN>* v, int64_t at, int n) {
 #pragma unroll
     for (int j = 0; j < kN; ++j) {
       const float u = v[0][j] - mu[j];
       const float dz = act_back<kAct>(v[1][j], __builtin_fmaf(u, gs[j], be[j]));
-      v[0].set(j, __builtin_fmaf(gs[j], dz, -__builtin_fmaf(u, k2[j], k1[j])));
+      v[0].set(j, __builtin_fmaf(gs[j], dz, -__builtin_fmaf(u * rs[j], k2[j], k1[j])));
     }
     T* p = static_cast<T*>(dx) + at;
     if (n == kN) v[0].store(p); else v[0].store(p, n);
@@ -815,13 +815,13 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d,
     return reinterpret_cast<const double2*>(ca)[g * d.Cg + i];
   }, [&](int g, double2 s) { sg[g] = make_float2((float)(s.y * inv_m), (float)(s.x * inv_m)); });
   __syncthreads();
-  // dx = gamma rstd dz - rstd s1 - (x - mean) rstd^2 s2
+  // dx = gamma rstd dz - rstd s1 - ((x - mean) rstd) (rstd s2)
   float k1[kA], k2[kA];
 #pragma unroll
   for (int j = 0; j < kA; ++j) {
     const float2 s = sg[(w.c + j) / d.Cg];
     k1[j] = rs[j] * s.x;
-    k2[j] = rs[j] * rs[j] * s.y;
+    k2[j] = rs[j] * s.y;
   }
   packed(raw);
   const Buf ro = w.over(d, dx);
@@ -832,8 +832,8 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_held(GroupNormDev d,
 #pragma unroll
     for (int j = 0; j < kN; ++j) {
       const int o = kOne ? 0 : j;
-      const float u = v[j] - mu[o];
-      v.set(j, __builtin_fmaf(gs[j], dz[i][j], -__builtin_fmaf(u, k2[o], k1[o])));
+      const float h = (v[j] - mu[o]) * rs[o];
+      v.set(j, __builtin_fmaf(gs[j], dz[i][j], -__builtin_fmaf(h, k2[o], k1[o])));
     }
     __builtin_amdgcn_raw_buffer_store_b128(raw_of<kType>(v), ro, w.at + i * w.step, 0, kAuxNT);
   }
@@ -970,11 +970,11 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_flat(GroupNormDev d,
   constexpr int kN = Elem<kType>::kVec;
   const Part<kN> w(d, blockIdx.x);
   Flat<kType, kR, 2> in(d, w, x, dy);
-  float mu[kN], gs[kN], be[kN], k1[kN], k2[kN];
+  float mu[kN], rs[kN], gs[kN], be[kN], k1[kN], k2[kN];
   w.channels(d, [&](int j, int c, int g) {
     mu[j] = mean[w.n * d.G + g];
-    k1[j] = rstd[w.n * d.G + g];
-    gs[j] = gamma[w.k * ld + c] * k1[j];
+    rs[j] = rstd[w.n * d.G + g];
+    gs[j] = gamma[w.k * ld + c] * rs[j];
     be[j] = beta[w.k * ld + c];
   });
   float a[kN] = {}, b[kN] = {};
@@ -1028,10 +1028,10 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_flat(GroupNormDev d,
     st[g] = make_float2((float)(s.y * inv_m), (float)(s.x * inv_m));
   });
   __syncthreads();
-  // dx = gamma rstd dz - rstd s1 - (x - mean) rstd^2 s2
+  // dx = gamma rstd dz - rstd s1 - ((x - mean) rstd) (rstd s2)
   w.channels(d, [&](int j, int, int g) {
-    k2[j] = k1[j] * k1[j] * st[g].y;
-    k1[j] *= st[g].x;
+    k1[j] = rs[j] * st[g].x;
+    k2[j] = rs[j] * st[g].y;
   });
   typedef typename Elem<kType>::T T;
 #pragma unroll
@@ -1040,8 +1040,8 @@ __global__ __launch_bounds__(kHeldThreads) void k_gn_bwd_flat(GroupNormDev d,
     auto v = in.v[i][0];
 #pragma unroll
     for (int j = 0; j < kN; ++j) {
-      const float u = v[j] - mu[j];
-      v.set(j, __builtin_fmaf(gs[j], dz[i][j], -__builtin_fmaf(u, k2[j], k1[j])));
+      const float h = (v[j] - mu[j]) * rs[j];
+      v.set(j, __builtin_fmaf(gs[j], dz[i][j], -__builtin_fmaf(h, k2[j], k1[j])));
     }
     T* p = static_cast<T*>(dx) + w.first + i * w.stride;
     if (n == kN) v.store(p); else v.store(p, n);
